@@ -382,6 +382,139 @@ int mx_rate_of_change_step(const void* x, int dtype, int64_t rows, int64_t cols,
                   float* x_prev, int init, void* workspace, size_t workspace_bytes,
                   double* result, void* stream);
 
+/* ---- between the linear layers: residual and norms, activations, 8-bit checkpoints ---- */
+
+/*
+ * 8-bit checkpoint of a matrix [rows x cols], for what a training step keeps between its forward and its backward pass.
+ * 1x32 groups along the columns (the last one of a row may be shorter) share S = 2^s, the smallest power of two that
+ * leaves no magnitude of the group above 448, s = ceil(log2(M / 448)), not below -127; an element is x / S rounded to the
+ * nearest OCP E4M3 value, ties to even, so that it comes back within 2^-4 of itself, or within 2^(s-10) near zero.
+ *     codes [r][j] = E4M3 code of element (r, j)      rows x P bytes, P = cols rounded up to a multiple of 32; the bytes
+ *     scales[r][g] = s + 127                          rows x P/32 bytes          past cols hold 0
+ *   values   device, dtype F32 or BF16, at the alignment of its elements, ld >= cols
+ *   codes    device, 8-byte aligned
+ *   1 <= cols, rows * P < 2^35.
+ * A NaN comes back as NaN; a group that holds an infinity comes back as NaN as a whole; a magnitude of 31/32 * 2^128 or more
+ * rounds to 2^128 and comes back as infinity.
+ */
+int mx_checkpoint_pack(const void* values, int dtype, int64_t rows, int64_t cols, int64_t ld,
+                  uint8_t* codes, uint8_t* scales, void* stream);
+int mx_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols,
+                  void* values, int dtype, int64_t ld, void* stream);
+
+/*
+ * The residual around a block of a transformer with the norms on both of its sides, in one pass.  x is the residual
+ * stream before the block, u the block's output:
+ *     v = post ? n(u; post_weight, post_bias) : u
+ *     h = residual_scale * x + branch_scale * gate . v          rounded to x's type
+ *     y = n(h; pre_weight, pre_bias)      (with pre)            of the rounded h: the next block's input
+ *   MX_NORM_RMS    n(a; w) = a r w,           r = 1 / sqrt(mean(a^2) + eps)          (biases are not read)
+ *   MX_NORM_LAYER  n(a; w, b) = (a - mean(a)) r w + b,   r = 1 / sqrt(var(a) + eps)
+ * FP32 throughout, sums included; the sum of the squares of a row must be finite.
+ *   x, u          device, [rows x cols]; x_dtype and u_dtype F32 or BF16, not a BF16 stream with an F32 branch
+ *                 (MX_ERR_DTYPE).  u NULL: no block, y = n(x); h, gate, post and the scales are not used then and h must be NULL
+ *   h             device out, x_dtype; may be x itself (with ldh = ldx)
+ *   y             device out, u_dtype; or NULL with
+ *   y_codes, y_scales   device out: y as MXFP4 row codes, the Q(1) of mx_quantize with round_D and scale_mode applied to
+ *                 the FP32 values, which is what mx_linear_fwd takes as xq, xs.  cols % 32 == 0; y_codes 16-byte aligned
+ *   *_weight, *_bias    device, cols values of param_dtype; NULL is 1 and 0
+ *   gate          device, gate_dtype, gate_rows rows with stride ld_gate, or NULL; gate_rows divides rows, and each gate
+ *                 row is that of rows / gate_rows consecutive rows (1: one for all; the number of sequences; rows)
+ *   h8, h8_scales, u8, u8_scales   device out, each pair or NULL: mx_checkpoint_pack of h and of u
+ *   stats         device out, FP32 [rows][4], 16-byte aligned, or NULL: mean and r of u, mean and r of h (0 where there is
+ *                 no such norm, or no mean), for the backward pass
+ * 1 <= cols <= 16384, rows * cols < 2^35; eps at least 2^-126 (MX_ERR_MODE); pointers at the alignment of their elements
+ * unless stated.  At least one of h and y is asked for.
+ */
+enum { MX_NORM_RMS = 0, MX_NORM_LAYER = 1 };
+typedef struct mx_residual_norm {
+    int64_t rows, cols;
+    const void* x;
+    const void* u;
+    void* h;
+    void* y;
+    int64_t ldx, ldu, ldh, ldy;
+    int x_dtype, u_dtype;
+    int norm;
+    int pre, post;
+    const void* pre_weight;
+    const void* pre_bias;
+    const void* post_weight;
+    const void* post_bias;
+    int param_dtype;
+    const void* gate;
+    int gate_dtype;
+    int64_t gate_rows, ld_gate;
+    float residual_scale, branch_scale, eps;
+    uint8_t* y_codes;
+    uint8_t* y_scales;
+    int scale_mode;
+    uint8_t* h8;
+    uint8_t* h8_scales;
+    uint8_t* u8;
+    uint8_t* u8_scales;
+    float* stats;
+} mx_residual_norm;
+int mx_residual_norm_fwd(const mx_residual_norm* p, void* stream);
+
+/*
+ * Gradients of mx_residual_norm_fwd from those of h and y.  With a^ = (a - mean) r at the forward pass's statistics
+ * ([...]: MX_NORM_LAYER only):
+ *     b = dy pre_weight;   t = dh + r_h (b - [mean(b)] - h^ mean(b h^));   dx = residual_scale * t
+ *     d = branch_scale * gate . t;   c = d post_weight;   du = post ? r_u (c - [mean(c)] - u^ mean(c u^)) : d
+ *     dpre_weight = sum dy h^, dpre_bias = sum dy, dpost_weight = sum d u^, dpost_bias = sum d   over the rows
+ *     dgate = sum branch_scale * t . v   over the rows of each gate row
+ *   p     the forward call's arguments.  Read of it: rows, cols, types, norm, pre, post, the parameters without pre_bias,
+ *         gate and scales, stats, and h and u as the forward pass left them, or h8 and u8 (with scales) in their place if
+ *         either is set.  h (x, where there is no block) is read if dy is given, u with post or dgate; else they may be
+ *         NULL.  branch tells whether there was a block.
+ *   dh, dy      device, x_dtype and u_dtype; one of them may be NULL and is zero then; dy needs pre
+ *   dx, du      device out, x_dtype and u_dtype, each or NULL
+ *   dpre_weight, dpre_bias, dpost_weight, dpost_bias   device out, cols values of param_dtype, each or NULL
+ *   dgate       device out, [gate_rows x cols] dense, gate_dtype, or NULL
+ *   workspace   device, 16-byte aligned, mx_residual_norm_workspace_bytes(rows, cols, gate_rows) bytes (gate_rows 0
+ *               without a gate); MX_ERR_WORKSPACE if NULL or smaller.  Not kept between calls, nothing is cleared.
+ * Sums over rows run in one fixed order for given sizes, so that a call repeats bit for bit.
+ */
+typedef struct mx_residual_norm_grads {
+    int branch;
+    const void* dh;
+    const void* dy;
+    void* dx;
+    void* du;
+    int64_t lddh, lddy, lddx, lddu;
+    void* dpre_weight;
+    void* dpre_bias;
+    void* dpost_weight;
+    void* dpost_bias;
+    void* dgate;
+    void* workspace;
+    size_t workspace_bytes;
+} mx_residual_norm_grads;
+size_t mx_residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_rows);
+int mx_residual_norm_bwd(const mx_residual_norm* p, const mx_residual_norm_grads* d, void* stream);
+
+/*
+ * Activation of an MLP between its two linear layers: a = act(p), p [rows x cols], or gated, p [rows x 2 cols],
+ *     a[:, j] = act(p[:, j]) * p[:, cols + j].
+ *   MX_ACT_GELU   x Phi(x), Phi the normal distribution function;   MX_ACT_SILU   x / (1 + exp(-x)).
+ * FP32; act(x) is within 2^-18 max(|act(x)|, 2^-100) of its exact value for |x| <= 4, and within 2^-15 of that beyond.
+ *   p        device, dtype F32 or BF16, row stride ldp
+ *   a        device out, dtype, row stride lda; or NULL with a_codes, a_scales: a as MXFP4 row codes (as y_codes above;
+ *            cols % 32 == 0, a_codes 16-byte aligned)
+ *   p8, p8_scales   device out, or NULL: the 8-bit checkpoint of p; gated, that of the matrix [2 rows x cols] whose rows
+ *            are the two halves of each row in turn
+ *   1 <= cols < 2^30, rows * cols < 2^35 (rounded up to whole groups); pointers at the alignment of their elements, p8 8 bytes.
+ * Backward: dp from da, with p as given or (p8 set) its checkpoint in the place of p:
+ *     dp = da act'(p);   gated, with p = [g | w]:   [da w act'(g) | da act(g)].
+ */
+enum { MX_ACT_GELU = 0, MX_ACT_SILU = 1 };
+int mx_activation_fwd(const void* p, int dtype, int64_t rows, int64_t cols, int64_t ldp, int kind, int gated,
+                  void* a, int64_t lda, uint8_t* a_codes, uint8_t* a_scales, int scale_mode,
+                  uint8_t* p8, uint8_t* p8_scales, void* stream);
+int mx_activation_bwd(const void* p, const uint8_t* p8, const uint8_t* p8_scales, int dtype, int64_t rows, int64_t cols,
+                  int64_t ldp, int kind, int gated, const void* da, int64_t ldda, void* dp, int64_t lddp, void* stream);
+
 /* ---- helpers (not part of the path) ---- */
 
 /* Bytes of workspace the product `which` (MX_GEMM_*) needs for these sizes. */

@@ -11,7 +11,9 @@ from .binding import (  # noqa: F401
     RampingAdamwState, mx_ramping_adamw_step,
     CALIBRATION_MFMA_OPERAND_BYTES, NOALLOC_MAX_WORKSPACE_BYTES, mx_calibration_copy, mx_calibration_mfma,
     mx_linear_bwd_dw_noalloc, mx_quantize_e3m0, mx_dequantize_e3m0, mx_linear_fwd_gelu_quant,
+    mx_checkpoint_pack, mx_checkpoint_unpack,
 )
+from .block import MxActivation, MxResidualNorm, activation, residual_norm  # noqa: F401
 from .layer import MxLinearStep  # noqa: F401
 from .module import MxLinear  # noqa: F401
 from .optim import QRampingAdamW  # noqa: F401

@@ -29,6 +29,8 @@ EXPORTS = ["mx_quantize", "mx_quantize_e3m0", "mx_dequantize_e3m0", "mx_quantize
            "mx_linear_bwd_dw", "mx_linear_bwd_dw_noalloc", "mx_ema_weight_quant", "mx_linear_workspace_bytes",
            "mx_oscillation_accumulate", "mx_ramping_factor",
            "mx_ramping_adamw_step", "mx_quant_confidence", "mx_rate_of_change_workspace_bytes", "mx_rate_of_change_step",
+           "mx_checkpoint_pack", "mx_checkpoint_unpack", "mx_residual_norm_fwd", "mx_residual_norm_bwd",
+           "mx_residual_norm_workspace_bytes", "mx_activation_fwd", "mx_activation_bwd",
            "mx_dequantize", "mx_calibration_copy", "mx_calibration_mfma", "mx_last_hip_error", "mx_version"]
 
 
@@ -41,6 +43,27 @@ class _TransposedJob(ctypes.Structure):
                 ("row_codes_in", ctypes.c_void_p), ("row_scales_in", ctypes.c_void_p),
                 ("seed", ctypes.c_uint64), ("index_base", ctypes.c_uint64), ("seed_dev", ctypes.c_void_p),
                 ("col_sums", ctypes.c_void_p), ("col_sum_workspace", ctypes.c_void_p)]
+
+
+class ResidualNormArgs(ctypes.Structure):
+    """mx_residual_norm of include/mxfp4.h."""
+    _fields_ = ([("rows", ctypes.c_int64), ("cols", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("x", "u", "h", "y")] +
+                [(n, ctypes.c_int64) for n in ("ldx", "ldu", "ldh", "ldy")] +
+                [(n, ctypes.c_int) for n in ("x_dtype", "u_dtype", "norm", "pre", "post")] +
+                [(n, ctypes.c_void_p) for n in ("pre_weight", "pre_bias", "post_weight", "post_bias")] +
+                [("param_dtype", ctypes.c_int), ("gate", ctypes.c_void_p), ("gate_dtype", ctypes.c_int),
+                 ("gate_rows", ctypes.c_int64), ("ld_gate", ctypes.c_int64)] +
+                [(n, ctypes.c_float) for n in ("residual_scale", "branch_scale", "eps")] +
+                [("y_codes", ctypes.c_void_p), ("y_scales", ctypes.c_void_p), ("scale_mode", ctypes.c_int)] +
+                [(n, ctypes.c_void_p) for n in ("h8", "h8_scales", "u8", "u8_scales", "stats")])
+
+
+class ResidualNormGrads(ctypes.Structure):
+    """mx_residual_norm_grads of include/mxfp4.h."""
+    _fields_ = ([("branch", ctypes.c_int)] + [(n, ctypes.c_void_p) for n in ("dh", "dy", "dx", "du")] +
+                [(n, ctypes.c_int64) for n in ("lddh", "lddy", "lddx", "lddu")] +
+                [(n, ctypes.c_void_p) for n in ("dpre_weight", "dpre_bias", "dpost_weight", "dpost_bias", "dgate", "workspace")] +
+                [("workspace_bytes", ctypes.c_size_t)])
 
 
 class MxError(RuntimeError):
@@ -103,6 +126,20 @@ def lib():
     L.mx_rate_of_change_workspace_bytes.argtypes = []
     L.mx_rate_of_change_step.restype = ci
     L.mx_rate_of_change_step.argtypes = [vp, ci, i64, i64, i64, vp, ci, vp, sz, vp, vp]
+    L.mx_checkpoint_pack.restype = ci
+    L.mx_checkpoint_pack.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp]
+    L.mx_checkpoint_unpack.restype = ci
+    L.mx_checkpoint_unpack.argtypes = [vp, vp, i64, i64, vp, ci, i64, vp]
+    L.mx_residual_norm_fwd.restype = ci
+    L.mx_residual_norm_fwd.argtypes = [vp, vp]
+    L.mx_residual_norm_bwd.restype = ci
+    L.mx_residual_norm_bwd.argtypes = [vp, vp, vp]
+    L.mx_residual_norm_workspace_bytes.restype = sz
+    L.mx_residual_norm_workspace_bytes.argtypes = [i64, i64, i64]
+    L.mx_activation_fwd.restype = ci
+    L.mx_activation_fwd.argtypes = [vp, ci, i64, i64, i64, ci, ci, vp, i64, vp, vp, ci, vp, vp, vp]
+    L.mx_activation_bwd.restype = ci
+    L.mx_activation_bwd.argtypes = [vp, vp, vp, ci, i64, i64, i64, ci, ci, vp, i64, vp, i64, vp]
     L.mx_dequantize.restype = ci
     L.mx_dequantize.argtypes = [vp, vp, i64, i64, vp, vp]
     L.mx_calibration_copy.restype = ci
@@ -512,6 +549,25 @@ def mx_rate_of_change_step(x, state, init=None, stream=None):
     _check("mx_rate_of_change_step", rc)
     state.started = True
     return state
+
+
+def mx_checkpoint_pack(src, out=None, stream=None):
+    """8-bit checkpoint of src [..., cols] (float32 or bfloat16).  Returns (codes[rows, P], scales[rows, P/32]), P = cols
+    rounded up to a multiple of 32."""
+    codes, scales = out if out is not None else (None, None)
+    return host().checkpoint_pack(src, codes, scales, -1 if stream is None else _stream(stream).value or 0)
+
+
+def mx_checkpoint_unpack(codes, scales, cols, dtype=torch.float32, out=None, stream=None):
+    """The values [rows, cols] that a checkpoint stands for."""
+    return host().checkpoint_unpack(codes, scales, cols, dtype == torch.bfloat16 or _not_f32(dtype), out,
+                                    -1 if stream is None else _stream(stream).value or 0)
+
+
+def _not_f32(dtype):
+    if dtype != torch.float32:
+        raise TypeError("values are float32 or bfloat16, got %s" % dtype)
+    return False
 
 
 def mx_dequantize(codes, scales, stream=None):

@@ -1,14 +1,16 @@
 """Compile the HIP sources under csrc/ for gfx950 into libmxfp4_hip.so, and the native host path of the Python front
 ends (csrc/mx_torch.cpp, against the installed torch) into _mx_torch.so, both in-tree."""
+import concurrent.futures
 import os
 import subprocess
 import sys
+import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libmxfp4_hip.so")
-SOURCES = ["mx_api.hip", "mx_quant.hip", "mx_gemm.hip", "mx_optim.hip"]
-HEADERS = ["mx_device.hpp", "mx_launch.hpp", os.path.join("..", "..", "include", "mxfp4.h")]
+SOURCES = ["mx_api.hip", "mx_quant.hip", "mx_gemm.hip", "mx_optim.hip", "mx_norm.hip", "mx_act.hip"]
+HEADERS = ["mx_device.hpp", "mx_block.hpp", "mx_launch.hpp", os.path.join("..", "..", "include", "mxfp4.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -47,14 +49,17 @@ def build(force=True, verbose=False, extra_flags=()):
     """Build the two shared libraries; returns the HIP library's path."""
     if not force and not is_stale():
         return LIB
-    cmd = [HIPCC] + FLAGS + list(extra_flags) + [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
-    cmd = host_command()
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+
+    with tempfile.TemporaryDirectory() as tmp, concurrent.futures.ThreadPoolExecutor(len(SOURCES)) as pool:   # one compiler for each source
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        compile_flags = [f for f in FLAGS if f != "-shared"] + ["-c"] + list(extra_flags)
+        list(pool.map(run, [[HIPCC] + compile_flags + [os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objects)]))
+        run([HIPCC] + FLAGS + objects + ["-o", LIB])
+    run(host_command())
     return LIB
 
 

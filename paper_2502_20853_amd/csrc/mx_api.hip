@@ -150,6 +150,79 @@ int check_gemm(const GemmParams& p)
     return MX_OK;
 }
 
+// Rows of `cols` elements at the alignment of their type.
+static int check_matrix(const void* p, bool bf16, int64_t rows, int64_t cols, int64_t ld)
+{
+    if (rows > 1 && ld < cols) return MX_ERR_SHAPE;
+    return aligned(p, bf16 ? 2 : 4) ? MX_OK : MX_ERR_ALIGN;
+}
+
+static bool too_many(int64_t rows, int64_t cols) { return rows > MAX_ELEMS / ((cols + 31) / 32 * 32); }
+
+int check_checkpoint(const CheckpointParams& p)
+{
+    if (p.rows <= 0 || p.cols <= 0 || p.cols >= (1LL << 30) || too_many(p.rows, p.cols)) return MX_ERR_SHAPE;
+    if (!aligned(p.codes, 8)) return MX_ERR_ALIGN;
+    return check_matrix(p.values, p.bf16, p.rows, p.cols, p.ld);
+}
+
+int check_activation(const ActivationParams& p, bool backward)
+{
+    if (p.rows <= 0 || p.cols <= 0 || p.cols >= (1LL << 30) || too_many(p.rows, p.cols)) return MX_ERR_SHAPE;
+    int rc = MX_OK;
+    if (p.p) rc = check_matrix(p.p, p.bf16, p.rows, p.gated ? 2 * p.cols : p.cols, p.ldp);
+    if (rc == MX_OK && p.a) rc = check_matrix(p.a, p.bf16, p.rows, p.cols, p.lda);
+    if (rc == MX_OK && backward) rc = check_matrix(p.dp, p.bf16, p.rows, p.gated ? 2 * p.cols : p.cols, p.lddp);
+    if (rc != MX_OK) return rc;
+    if (p.a_codes) {
+        if (p.cols % 32 != 0) return MX_ERR_SHAPE;
+        if (!aligned(p.a_codes, 16)) return MX_ERR_ALIGN;
+    }
+    return aligned(p.p8, 8) ? MX_OK : MX_ERR_ALIGN;
+}
+
+int check_residual_norm(const ResidualNormParams& p)
+{
+    if (p.rows <= 0 || p.cols <= 0 || p.cols > RESIDUAL_NORM_MAX_COLS || too_many(p.rows, p.cols)) return MX_ERR_SHAPE;
+    if (p.x_bf16 && !p.u_bf16) return MX_ERR_DTYPE;
+    // written so that NaN fails
+    if (!(p.eps >= 1.17549435e-38f && p.eps < 1e30f) || !(p.residual_scale - p.residual_scale == 0.0f) ||
+        !(p.branch_scale - p.branch_scale == 0.0f)) return MX_ERR_MODE;
+    if (!p.branch && (p.gate || p.post || !p.pre)) return MX_ERR_MODE;
+    int rc = MX_OK;
+    if (p.x) rc = check_matrix(p.x, p.x_bf16, p.rows, p.cols, p.ldx);
+    if (rc == MX_OK && p.u) rc = check_matrix(p.u, p.u_bf16, p.rows, p.cols, p.ldu);
+    if (rc == MX_OK && p.h) rc = check_matrix(p.h, p.x_bf16, p.rows, p.cols, p.ldh);
+    if (rc == MX_OK && p.y) rc = check_matrix(p.y, p.u_bf16, p.rows, p.cols, p.ldy);
+    if (rc != MX_OK) return rc;
+    for (const void* w : {p.pre_weight, p.pre_bias, p.post_weight, p.post_bias})
+        if (!aligned(w, p.param_bf16 ? 2 : 4)) return MX_ERR_ALIGN;
+    if (p.gate) {
+        if (p.gate_rows <= 0 || p.rows % p.gate_rows != 0 || (p.gate_rows > 1 && p.ld_gate < p.cols)) return MX_ERR_SHAPE;
+        if (!aligned(p.gate, p.gate_bf16 ? 2 : 4)) return MX_ERR_ALIGN;
+    }
+    if (p.y_codes) {
+        if (p.cols % 32 != 0) return MX_ERR_SHAPE;
+        if (!aligned(p.y_codes, 16)) return MX_ERR_ALIGN;
+    }
+    if (!aligned(p.h8, 8) || !aligned(p.u8, 8) || !aligned(p.stats, 16)) return MX_ERR_ALIGN;
+    return MX_OK;
+}
+
+int check_residual_norm_grads(const ResidualNormParams& p, const ResidualNormGrads& d)
+{
+    int rc = MX_OK;
+    if (d.dh) rc = check_matrix(d.dh, p.x_bf16, p.rows, p.cols, d.lddh);
+    if (rc == MX_OK && d.dy) rc = check_matrix(d.dy, p.u_bf16, p.rows, p.cols, d.lddy);
+    if (rc == MX_OK && d.dx) rc = check_matrix(d.dx, p.x_bf16, p.rows, p.cols, d.lddx);
+    if (rc == MX_OK && d.du) rc = check_matrix(d.du, p.u_bf16, p.rows, p.cols, d.lddu);
+    if (rc != MX_OK) return rc;
+    for (const void* w : {d.dpre_weight, d.dpre_bias, d.dpost_weight, d.dpost_bias})
+        if (!aligned(w, p.param_bf16 ? 2 : 4)) return MX_ERR_ALIGN;
+    if (!aligned(d.dgate, p.gate_bf16 ? 2 : 4) || !aligned(d.workspace, 16)) return MX_ERR_ALIGN;
+    return MX_OK;
+}
+
 }  // namespace mxl
 
 extern "C" {
@@ -453,6 +526,138 @@ int mx_rate_of_change_step(const void* x, int dtype, int64_t rows, int64_t cols,
     p.x = x; p.bf16 = dtype == MX_DTYPE_BF16; p.rows = rows; p.cols = cols; p.ld = ld;
     p.x_prev = x_prev; p.init = init; p.partial = static_cast<double*>(workspace); p.result = result;
     return hip_status(mxl::launch_rate_of_change(p, static_cast<hipStream_t>(stream)));
+}
+
+static bool is_dtype(int d) { return d == MX_DTYPE_F32 || d == MX_DTYPE_BF16; }
+static bool half_set(const void* a, const void* b) { return (a == nullptr) != (b == nullptr); }
+
+static int checkpoint_call(const void* values, int dtype, int64_t rows, int64_t cols, int64_t ld,
+                  const uint8_t* codes, const uint8_t* scales, bool pack, void* stream)
+{
+    if (!values || !codes || !scales) return MX_ERR_NULL;
+    if (!is_dtype(dtype)) return MX_ERR_DTYPE;
+    const mxl::CheckpointParams p{const_cast<void*>(values), dtype == MX_DTYPE_BF16, rows, cols, ld, const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales)};
+    const int rc = mxl::check_checkpoint(p);
+    if (rc != MX_OK) return rc;
+    return hip_status(pack ? mxl::launch_checkpoint_pack(p, static_cast<hipStream_t>(stream)) : mxl::launch_checkpoint_unpack(p, static_cast<hipStream_t>(stream)));
+}
+
+int mx_checkpoint_pack(const void* values, int dtype, int64_t rows, int64_t cols, int64_t ld,
+                  uint8_t* codes, uint8_t* scales, void* stream)
+{
+    return checkpoint_call(values, dtype, rows, cols, ld, codes, scales, true, stream);
+}
+
+int mx_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols,
+                  void* values, int dtype, int64_t ld, void* stream)
+{
+    return checkpoint_call(values, dtype, rows, cols, ld, codes, scales, false, stream);
+}
+
+static int residual_norm_params(const mx_residual_norm& a, bool branch, mxl::ResidualNormParams& p)
+{
+    if (!is_dtype(a.x_dtype) || !is_dtype(a.u_dtype) || !is_dtype(a.param_dtype) || (a.gate && !is_dtype(a.gate_dtype))) return MX_ERR_DTYPE;
+    if ((a.norm != MX_NORM_RMS && a.norm != MX_NORM_LAYER) || (a.pre != 0 && a.pre != 1) || (a.post != 0 && a.post != 1)) return MX_ERR_MODE;
+    p = mxl::ResidualNormParams{};
+    p.x = a.x; p.u = a.u; p.h = a.h; p.y = a.y; p.ldx = a.ldx; p.ldu = a.ldu; p.ldh = a.ldh; p.ldy = a.ldy;
+    p.x_bf16 = a.x_dtype == MX_DTYPE_BF16; p.u_bf16 = a.u_dtype == MX_DTYPE_BF16;
+    p.rows = a.rows; p.cols = a.cols;
+    p.layer = a.norm == MX_NORM_LAYER; p.branch = branch; p.pre = a.pre == 1; p.post = a.post == 1;
+    p.pre_weight = a.pre_weight; p.pre_bias = a.pre_bias; p.post_weight = a.post_weight; p.post_bias = a.post_bias;
+    p.param_bf16 = a.param_dtype == MX_DTYPE_BF16;
+    p.gate = a.gate; p.gate_bf16 = a.gate_dtype == MX_DTYPE_BF16; p.gate_rows = a.gate_rows; p.ld_gate = a.ld_gate;
+    p.residual_scale = a.residual_scale; p.branch_scale = a.branch_scale; p.eps = a.eps;
+    p.y_codes = a.y_codes; p.y_scales = a.y_scales; p.floor_mode = a.scale_mode == MX_SCALE_FLOOR;
+    p.h8 = a.h8; p.h8_scales = a.h8_scales; p.u8 = a.u8; p.u8_scales = a.u8_scales; p.stats = a.stats;
+    return MX_OK;
+}
+
+int mx_residual_norm_fwd(const mx_residual_norm* a, void* stream)
+{
+    if (!a || !a->x) return MX_ERR_NULL;
+    if (half_set(a->y_codes, a->y_scales) || half_set(a->h8, a->h8_scales) || half_set(a->u8, a->u8_scales)) return MX_ERR_NULL;
+    if (!a->u && a->h) return MX_ERR_NULL;
+    if (a->u && !a->h) return MX_ERR_NULL;
+    if (a->pre && !a->y && !a->y_codes) return MX_ERR_NULL;
+    if (!a->u && a->u8) return MX_ERR_NULL;
+    if ((a->y && a->y_codes) || (!a->pre && (a->y || a->y_codes))) return MX_ERR_MODE;
+    if (a->y_codes && a->scale_mode != MX_SCALE_TRUNCFREE && a->scale_mode != MX_SCALE_FLOOR) return MX_ERR_MODE;
+    mxl::ResidualNormParams p;
+    int rc = residual_norm_params(*a, a->u != nullptr, p);
+    if (rc == MX_OK) rc = mxl::check_residual_norm(p);
+    if (rc != MX_OK) return rc;
+    return hip_status(mxl::launch_residual_norm_fwd(p, static_cast<hipStream_t>(stream)));
+}
+
+size_t mx_residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_rows)
+{
+    if (rows <= 0 || cols <= 0 || gate_rows < 0 || gate_rows > rows) return 0;
+    return mxl::residual_norm_workspace_bytes(rows, cols, gate_rows);
+}
+
+int mx_residual_norm_bwd(const mx_residual_norm* a, const mx_residual_norm_grads* b, void* stream)
+{
+    if (!a || !b || (!b->dh && !b->dy) || !a->stats) return MX_ERR_NULL;
+    if (half_set(a->h8, a->h8_scales) || half_set(a->u8, a->u8_scales)) return MX_ERR_NULL;
+    if ((b->branch != 0 && b->branch != 1) || (b->dy && !a->pre)) return MX_ERR_MODE;
+    if (!b->branch && (b->du || b->dgate)) return MX_ERR_MODE;
+    if (b->dgate && !a->gate) return MX_ERR_NULL;
+    const bool eight = a->h8 || a->u8;
+    mxl::ResidualNormParams p;
+    int rc = residual_norm_params(*a, b->branch == 1, p);
+    if (rc != MX_OK) return rc;
+    if (!b->branch && !eight) { p.h = const_cast<void*>(a->x); p.ldh = a->ldx; }
+    if (b->dy && !(eight ? (const void*)a->h8 : p.h)) return MX_ERR_NULL;
+    if ((a->post || b->dgate) && !(eight ? (const void*)a->u8 : a->u)) return MX_ERR_NULL;
+    p.x = nullptr; p.y = nullptr; p.y_codes = nullptr;
+    rc = mxl::check_residual_norm(p);
+    if (rc != MX_OK) return rc;
+    const mxl::ResidualNormGrads d{b->dh, b->dy, b->dx, b->du, b->lddh, b->lddy, b->lddx, b->lddu, b->dpre_weight, b->dpre_bias,
+                                   b->dpost_weight, b->dpost_bias, b->dgate, b->workspace};
+    if (!b->workspace || b->workspace_bytes < mxl::residual_norm_workspace_bytes(p.rows, p.cols, p.gate ? p.gate_rows : 0)) return MX_ERR_WORKSPACE;
+    rc = mxl::check_residual_norm_grads(p, d);
+    if (rc != MX_OK) return rc;
+    return hip_status(mxl::launch_residual_norm_bwd(p, d, static_cast<hipStream_t>(stream)));
+}
+
+static int activation_params(int dtype, int64_t rows, int64_t cols, int kind, int gated, mxl::ActivationParams& q)
+{
+    if (!is_dtype(dtype)) return MX_ERR_DTYPE;
+    if ((kind != MX_ACT_GELU && kind != MX_ACT_SILU) || (gated != 0 && gated != 1)) return MX_ERR_MODE;
+    q = mxl::ActivationParams{};
+    q.bf16 = dtype == MX_DTYPE_BF16; q.rows = rows; q.cols = cols; q.silu = kind == MX_ACT_SILU; q.gated = gated == 1;
+    return MX_OK;
+}
+
+int mx_activation_fwd(const void* p, int dtype, int64_t rows, int64_t cols, int64_t ldp, int kind, int gated,
+                  void* a, int64_t lda, uint8_t* a_codes, uint8_t* a_scales, int scale_mode,
+                  uint8_t* p8, uint8_t* p8_scales, void* stream)
+{
+    if (!p || (!a && !a_codes) || half_set(a_codes, a_scales) || half_set(p8, p8_scales)) return MX_ERR_NULL;
+    if (a && a_codes) return MX_ERR_MODE;
+    if (a_codes && scale_mode != MX_SCALE_TRUNCFREE && scale_mode != MX_SCALE_FLOOR) return MX_ERR_MODE;
+    mxl::ActivationParams q;
+    int rc = activation_params(dtype, rows, cols, kind, gated, q);
+    if (rc != MX_OK) return rc;
+    q.p = p; q.ldp = ldp; q.a = a; q.lda = lda; q.a_codes = a_codes; q.a_scales = a_scales; q.floor_mode = scale_mode == MX_SCALE_FLOOR;
+    q.p8 = p8; q.p8_scales = p8_scales;
+    rc = mxl::check_activation(q, false);
+    if (rc != MX_OK) return rc;
+    return hip_status(mxl::launch_activation_fwd(q, static_cast<hipStream_t>(stream)));
+}
+
+int mx_activation_bwd(const void* p, const uint8_t* p8, const uint8_t* p8_scales, int dtype, int64_t rows, int64_t cols,
+                  int64_t ldp, int kind, int gated, const void* da, int64_t ldda, void* dp, int64_t lddp, void* stream)
+{
+    if ((!p && !p8) || half_set(p8, p8_scales) || !da || !dp) return MX_ERR_NULL;
+    mxl::ActivationParams q;
+    int rc = activation_params(dtype, rows, cols, kind, gated, q);
+    if (rc != MX_OK) return rc;
+    q.p = p8 ? nullptr : p; q.ldp = ldp; q.a = const_cast<void*>(da); q.lda = ldda; q.dp = dp; q.lddp = lddp;
+    q.p8 = const_cast<uint8_t*>(p8); q.p8_scales = const_cast<uint8_t*>(p8_scales);
+    rc = mxl::check_activation(q, true);
+    if (rc != MX_OK) return rc;
+    return hip_status(mxl::launch_activation_bwd(q, static_cast<hipStream_t>(stream)));
 }
 
 int mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols,

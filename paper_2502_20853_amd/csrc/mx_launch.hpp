@@ -192,6 +192,86 @@ constexpr int WINDOW_BATCH_MAX = 24;
 hipError_t launch_ramping_window_batch(const RampingWindowParams& p, const WindowTensor* tensors, const int64_t* counts,
                                        const bool* grad_bf16, int count, hipStream_t st);
 
+// h = residual_scale x + branch_scale gate . post(u), y = pre(h); see mx_residual_norm_fwd.  What a pass does not read or
+// write is null.  The backward pass takes h and u (or their 8-bit codes) and the statistics of the forward pass.
+struct ResidualNormParams {
+    const void* x;
+    const void* u;
+    void* h;
+    void* y;
+    int64_t ldx, ldu, ldh, ldy;
+    bool x_bf16, u_bf16;       // h is of x's type, y of u's; bf16 stream with FP32 branch is not taken
+    int64_t rows, cols;
+    bool layer, branch, pre, post;
+    const void* pre_weight;
+    const void* pre_bias;
+    const void* post_weight;
+    const void* post_bias;
+    bool param_bf16;
+    const void* gate;
+    bool gate_bf16;
+    int64_t gate_rows, ld_gate;
+    float residual_scale, branch_scale, eps;
+    uint8_t* y_codes;          // y as MXFP4 codes and scale bytes instead of values
+    uint8_t* y_scales;
+    bool floor_mode;
+    uint8_t* h8;               // 8-bit checkpoints of h and u
+    uint8_t* h8_scales;
+    uint8_t* u8;
+    uint8_t* u8_scales;
+    float* stats;              // [rows][4]: mean and reciprocal deviation of u, of h
+};
+struct ResidualNormGrads {
+    const void* dh;
+    const void* dy;
+    void* dx;
+    void* du;
+    int64_t lddh, lddy, lddx, lddu;
+    void* dpre_weight;
+    void* dpre_bias;
+    void* dpost_weight;
+    void* dpost_bias;
+    void* dgate;               // [gate_rows][cols], dense
+    void* workspace;           // residual_norm_workspace_bytes
+};
+constexpr int64_t RESIDUAL_NORM_MAX_COLS = 16384;
+int check_residual_norm(const ResidualNormParams& p);
+int check_residual_norm_grads(const ResidualNormParams& p, const ResidualNormGrads& d);    // without the workspace's size
+hipError_t launch_residual_norm_fwd(const ResidualNormParams& p, hipStream_t st);
+size_t residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_rows);
+hipError_t launch_residual_norm_bwd(const ResidualNormParams& p, const ResidualNormGrads& d, hipStream_t st);
+
+// a = act(p), or act(p[:, :cols]) . p[:, cols:]; see mx_activation_fwd.
+struct ActivationParams {
+    const void* p;
+    void* a;                   // forward: out; backward: the output's gradient
+    void* dp;                  // backward: out
+    int64_t ldp, lda, lddp;
+    bool bf16;
+    int64_t rows, cols;        // of a
+    bool silu, gated;
+    uint8_t* a_codes;          // a as MXFP4 codes and scale bytes instead of values
+    uint8_t* a_scales;
+    bool floor_mode;
+    uint8_t* p8;               // 8-bit checkpoint of p: forward out (or null), backward in
+    uint8_t* p8_scales;
+};
+int check_activation(const ActivationParams& p, bool backward);
+hipError_t launch_activation_fwd(const ActivationParams& p, hipStream_t st);
+hipError_t launch_activation_bwd(const ActivationParams& p, hipStream_t st);
+
+// 8-bit checkpoint of a matrix and back.
+struct CheckpointParams {
+    void* values;              // pack: in; unpack: out
+    bool bf16;
+    int64_t rows, cols, ld;
+    uint8_t* codes;
+    uint8_t* scales;
+};
+int check_checkpoint(const CheckpointParams& p);
+hipError_t launch_checkpoint_pack(const CheckpointParams& p, hipStream_t st);
+hipError_t launch_checkpoint_unpack(const CheckpointParams& p, hipStream_t st);
+
 hipError_t launch_calibration_copy(void* dst, const void* src, size_t bytes, hipStream_t st);
 
 // Register-resident MFMA loop (calibration of the matrix pipe's sustained rate on given operand bytes).

@@ -9,6 +9,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 
 #include "../../include/mxfp4.h"
 #include "mx_launch.hpp"
@@ -495,6 +496,564 @@ void step_backward(const Tensor& dY, int64_t N, int64_t D, int64_t C, uint64_t s
     check_hip(mxl::launch_gemm_pair(pw, px, st), "mx_linear_bwd_dw");
 }
 
+// ---- between the linear layers: 8-bit checkpoints, residual and norms, activations ----
+
+int dtype_of(const Tensor& t) { return is_bf16(t) ? MX_DTYPE_BF16 : MX_DTYPE_F32; }
+
+// A tensor [..., cols] as rows of unit column stride: itself where it is such a matrix, a dense copy where it is not.
+struct Rows {
+    Tensor t;
+    int64_t rows, cols, ld;
+};
+Rows rows_of(const Tensor& in, int64_t cols)
+{
+    const int64_t rows = cols > 0 ? in.numel() / cols : 0;
+    if (in.dim() == 2 && in.size(1) > 0 && (in.size(1) == 1 || in.stride(1) == 1) && (rows <= 1 || in.stride(0) >= cols))
+        return {in, rows, cols, rows <= 1 ? cols : in.stride(0)};
+    return {in.contiguous(), rows, cols, cols};
+}
+
+void no_trace(const char* what)
+{
+    // a trace would record the allocations and none of the kernels, which are launched past the dispatcher
+    TORCH_CHECK_NOT_IMPLEMENTED(!torch::jit::tracer::isTracing(), what, " cannot be traced");
+}
+
+void no_tangent(const char* what, std::initializer_list<const OptTensor*> tensors)
+{
+    for (const OptTensor* t : tensors)
+        TORCH_CHECK_NOT_IMPLEMENTED(!*t || !(**t)._fw_grad(0).defined(), what, " has no forward-mode derivative");
+}
+
+// Runs a backward pass: a Python error reaches the caller of backward() as it is, any other exception as a RuntimeError.
+template <typename F>
+torch::autograd::variable_list carried(const char* what, F&& f)
+{
+    TORCH_CHECK_NOT_IMPLEMENTED(!at::GradMode::is_enabled(), what, " has no second derivative (create_graph)");
+    try {
+        at::AutoDispatchBelowADInplaceOrView guard;
+        return f();
+    } catch (const Status& s) {
+        py::gil_scoped_acquire gil;
+        raise_in_python(s);
+        python_error e;
+        e.persist();
+        throw e;
+    }
+}
+
+hipStream_t stream_of(const Tensor& t) { return c10::hip::getCurrentHIPStream(t.get_device()).stream(); }
+
+int64_t padded32(int64_t cols) { return round_up(cols, 32); }
+
+// [codes | scale bytes] of a checkpoint of rows x cols in a byte buffer.
+struct Eight {
+    int64_t codes, scales;
+};
+Eight carve8(Carver& c, int64_t rows, int64_t cols) { return {c.take(rows * padded32(cols)), c.take(rows * (padded32(cols) / 32))}; }
+
+hipStream_t given_stream(const Tensor& t, int64_t stream) { return stream == -1 ? stream_of(t) : reinterpret_cast<hipStream_t>(stream); }
+
+void check_codes(const Tensor& codes, const Tensor& scales, int64_t rows, int64_t cols, const Tensor& like)
+{
+    TORCH_CHECK_VALUE(codes.scalar_type() == at::kByte && scales.scalar_type() == at::kByte && codes.is_contiguous() && scales.is_contiguous() &&
+                      codes.numel() == rows * padded32(cols) && scales.numel() == rows * (padded32(cols) / 32),
+                      "a checkpoint of [", rows, ", ", cols, "] is contiguous uint8 codes [", rows, ", ", padded32(cols), "] and scales [", rows, ", ", padded32(cols) / 32, "]");
+    TORCH_CHECK(codes.get_device() == like.get_device() && scales.get_device() == like.get_device(), "codes, scales and values must be on one GPU");
+}
+
+std::pair<Tensor, Tensor> checkpoint_pack(const Tensor& src, const OptTensor& codes_out, const OptTensor& scales_out, int64_t stream)
+{
+    const char* fn = "mx_checkpoint_pack";
+    no_trace(fn);
+    const bool bf16 = is_bf16(src);
+    if (src.dim() < 1 || src.numel() == 0) throw Status(fn, MX_ERR_SHAPE);
+    at::AutoDispatchBelowADInplaceOrView guard;
+    const Rows r = rows_of(src, src.size(-1));
+    mxl::CheckpointParams p{r.t.data_ptr(), bf16, r.rows, r.cols, r.ld, nullptr, nullptr};
+    check(mxl::check_checkpoint(p), fn);
+    TORCH_CHECK(src.is_cuda(), fn, " runs on the GPU");
+    c10::hip::HIPGuard device((c10::DeviceIndex)src.get_device());
+    TORCH_CHECK_VALUE(codes_out.has_value() == scales_out.has_value(), "out is a pair (codes, scales)");
+    const Tensor codes = codes_out ? *codes_out : at::empty({r.rows, padded32(r.cols)}, src.options().dtype(at::kByte));
+    const Tensor scales = scales_out ? *scales_out : at::empty({r.rows, padded32(r.cols) / 32}, src.options().dtype(at::kByte));
+    check_codes(codes, scales, r.rows, r.cols, src);
+    p.codes = codes.data_ptr<uint8_t>(); p.scales = scales.data_ptr<uint8_t>();
+    check(mxl::check_checkpoint(p), fn);
+    check_hip(mxl::launch_checkpoint_pack(p, given_stream(src, stream)), fn);
+    return {codes, scales};
+}
+
+Tensor checkpoint_unpack(const Tensor& codes, const Tensor& scales, int64_t cols, bool bf16, const OptTensor& out, int64_t stream)
+{
+    const char* fn = "mx_checkpoint_unpack";
+    no_trace(fn);
+    if (cols <= 0 || codes.numel() == 0 || codes.dim() < 1) throw Status(fn, MX_ERR_SHAPE);
+    const int64_t rows = codes.numel() / codes.size(-1);
+    TORCH_CHECK_VALUE(codes.size(-1) == padded32(cols), "codes of ", cols, " columns have rows of ", padded32(cols));
+    check_codes(codes, scales, rows, cols, codes);
+    const at::ScalarType type = bf16 ? at::kBFloat16 : at::kFloat;
+    TORCH_CHECK_VALUE(!out || (out->dim() == 2 && out->size(0) == rows && out->size(1) == cols && (cols == 1 || out->stride(1) == 1) && out->scalar_type() == type),
+                      "out must be a [", rows, ", ", cols, "] matrix of the given type with unit column stride");
+    TORCH_CHECK(codes.is_cuda(), fn, " runs on the GPU");
+    TORCH_CHECK(!out || out->get_device() == codes.get_device(), "codes, scales and values must be on one GPU");
+    at::AutoDispatchBelowADInplaceOrView guard;
+    c10::hip::HIPGuard device((c10::DeviceIndex)codes.get_device());
+    const Tensor values = out ? *out : at::empty({rows, cols}, codes.options().dtype(type));
+    const mxl::CheckpointParams p{values.data_ptr(), bf16, rows, cols, rows > 1 ? values.stride(0) : cols, codes.data_ptr<uint8_t>(), scales.data_ptr<uint8_t>()};
+    check(mxl::check_checkpoint(p), fn);
+    check_hip(mxl::launch_checkpoint_unpack(p, given_stream(codes, stream)), fn);
+    return values;
+}
+
+struct NormOptions {
+    bool layer, pre, post, floor_mode;
+    float residual_scale, branch_scale, eps;
+};
+
+struct NormInputs {
+    Tensor x;
+    OptTensor u, pre_weight, pre_bias, post_weight, post_bias, gate;
+};
+
+constexpr const char* NORM = "residual_norm";
+
+// The gate as rows: one for all, one for each run of the rows of a matrix, or the leading sizes of x followed by ones.
+int64_t gate_rows_of(const Tensor& gate, const Tensor& x)
+{
+    const int64_t D = x.size(-1);
+    TORCH_CHECK_VALUE(gate.dim() >= 1 && gate.size(-1) == D, "gate: rows of ", D, " values expected, got ", gate.sizes());
+    const int64_t rows = gate.numel() / D;
+    if (rows == 1) return 1;
+    if (x.dim() == 2 && gate.dim() == 2) {
+        TORCH_CHECK_VALUE(rows > 0 && x.size(0) % rows == 0, "gate: ", rows, " rows do not divide ", x.size(0));
+        return rows;
+    }
+    bool fits = gate.dim() == x.dim(), ones = false;
+    for (int64_t i = 0; fits && i + 1 < gate.dim(); ++i) {
+        if (gate.size(i) != x.size(i)) ones = true;
+        fits = ones ? gate.size(i) == 1 : true;
+    }
+    TORCH_CHECK_VALUE(fits, "gate: its leading sizes must be those of x, ", x.sizes(), ", up to some dimension and ones behind it, got ", gate.sizes());
+    return rows;
+}
+
+const Tensor dense(const OptTensor& t) { return t ? t->contiguous() : Tensor(); }
+const void* data_of(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// Everything of a call but its outputs; the tensors it points into live in `keep`.
+mxl::ResidualNormParams norm_params(const NormInputs& in, const NormOptions& o, std::vector<Tensor>& keep)
+{
+    const Tensor& x = in.x;
+    const int64_t D = x.size(-1);
+    mxl::ResidualNormParams p{};
+    const Rows xr = rows_of(x, D);
+    keep.push_back(xr.t);
+    p.x = xr.t.data_ptr(); p.ldx = xr.ld; p.x_bf16 = is_bf16(x);
+    p.rows = xr.rows; p.cols = D;
+    p.u_bf16 = p.x_bf16;
+    p.branch = in.u.has_value();
+    if (in.u) {
+        const Rows ur = rows_of(*in.u, D);
+        keep.push_back(ur.t);
+        p.u = ur.t.data_ptr(); p.ldu = ur.ld; p.u_bf16 = is_bf16(*in.u);
+    }
+    p.layer = o.layer; p.pre = o.pre; p.post = o.post; p.floor_mode = o.floor_mode;
+    auto param = [&](const OptTensor& t, const char* name) -> const void* {
+        if (!t) return nullptr;
+        TORCH_CHECK_VALUE(t->dim() == 1 && t->size(0) == D, name, " must have ", D, " values");
+        keep.push_back(t->contiguous());
+        return keep.back().data_ptr();
+    };
+    p.pre_weight = param(in.pre_weight, "pre_weight"); p.pre_bias = param(in.pre_bias, "pre_bias");
+    p.post_weight = param(in.post_weight, "post_weight"); p.post_bias = param(in.post_bias, "post_bias");
+    bool first = true;
+    for (const OptTensor* t : {&in.pre_weight, &in.pre_bias, &in.post_weight, &in.post_bias}) {
+        if (!*t) continue;
+        const bool b = is_bf16(**t);
+        TORCH_CHECK_TYPE(first || b == p.param_bf16, "the norms' weights and biases must have one type");
+        p.param_bf16 = b;
+        first = false;
+    }
+    if (in.gate) {
+        p.gate_rows = gate_rows_of(*in.gate, x);
+        // rows of any stride where the gate is a matrix (one of several chunks of a projection, say)
+        const Rows gr = rows_of(in.gate->dim() == 2 ? *in.gate : in.gate->reshape({p.gate_rows, D}), D);
+        keep.push_back(gr.t);
+        p.gate = gr.t.data_ptr(); p.ld_gate = gr.ld; p.gate_bf16 = is_bf16(*in.gate);
+    }
+    p.residual_scale = o.residual_scale; p.branch_scale = o.branch_scale; p.eps = o.eps;
+    return p;
+}
+
+void check_norm_call(const NormInputs& in, const NormOptions& o, bool packed)
+{
+    no_trace(NORM);
+    const OptTensor x = in.x;
+    no_tangent(NORM, {&x, &in.u, &in.pre_weight, &in.pre_bias, &in.post_weight, &in.post_bias, &in.gate});
+    TORCH_CHECK_VALUE(in.x.dim() >= 1 && (!in.u || in.u->sizes() == in.x.sizes()), "u must have the sizes of x, ", in.x.sizes());
+    TORCH_CHECK_VALUE(in.u || (!in.gate && !o.post && o.pre && o.residual_scale == 1.0f && o.branch_scale == 1.0f),
+                      "without a branch u there is only the norm of x: no gate, scales or post-norm");
+    TORCH_CHECK_VALUE(o.pre || (!in.pre_weight && !in.pre_bias && !packed), "pre=False takes no pre_weight, pre_bias or packed");
+    TORCH_CHECK_VALUE(o.post || (!in.post_weight && !in.post_bias), "post=False takes no post_weight or post_bias");
+    TORCH_CHECK_VALUE(o.layer || (!in.pre_bias && !in.post_bias), "an RMS norm has no bias");
+    if (in.x.numel() == 0) throw Status("mx_residual_norm_fwd", MX_ERR_SHAPE);
+    std::vector<Tensor> keep;
+    mxl::ResidualNormParams p = norm_params(in, o, keep);
+    check(mxl::check_residual_norm(p), "mx_residual_norm_fwd");
+    if (packed && p.cols % 32 != 0) throw Status("mx_residual_norm_fwd", MX_ERR_SHAPE);
+    TORCH_CHECK(in.x.is_cuda(), NORM, " runs on the GPU");
+    for (const OptTensor* t : {&in.u, &in.pre_weight, &in.pre_bias, &in.post_weight, &in.post_bias, &in.gate})
+        TORCH_CHECK(!*t || (*t)->get_device() == in.x.get_device(), NORM, ": x, u, parameters and gate must be on one GPU");
+}
+
+// What a forward pass leaves for the backward pass.
+struct NormKept {
+    Tensor stats, eight;       // FP32 [rows][4]; [h8 | scales | u8 | scales]
+    Tensor h;                  // the stored stream (x itself without a branch)
+};
+
+struct NormEight {
+    Eight h{}, u{};
+    int64_t bytes = 0;
+    NormEight(int64_t rows, int64_t cols, bool with_h, bool with_u)
+    {
+        Carver c;
+        if (with_h) h = carve8(c, rows, cols);
+        if (with_u) u = carve8(c, rows, cols);
+        bytes = c.used;
+    }
+};
+
+// Outputs {h or undefined, y or undefined}, packed {h, codes, scales}.
+torch::autograd::variable_list norm_forward(const NormInputs& in, const NormOptions& o, bool packed, bool eight, NormKept* kept)
+{
+    std::vector<Tensor> keep;
+    mxl::ResidualNormParams p = norm_params(in, o, keep);
+    torch::autograd::variable_list out;
+    Tensor h, y;
+    if (p.branch) {
+        h = at::empty(in.x.sizes(), in.x.options());
+        p.h = h.data_ptr(); p.ldh = p.cols;
+    }
+    out.push_back(h);
+    if (p.pre && packed) {
+        const Tensor codes = at::empty({p.rows, p.cols / 2}, in.x.options().dtype(at::kByte)), scales = at::empty({p.rows, p.cols / 32}, in.x.options().dtype(at::kByte));
+        p.y_codes = codes.data_ptr<uint8_t>(); p.y_scales = scales.data_ptr<uint8_t>();
+        out.push_back(codes);
+        out.push_back(scales);
+    } else if (p.pre) {
+        y = at::empty(in.x.sizes(), (in.u ? *in.u : in.x).options());
+        p.y = y.data_ptr(); p.ldy = p.cols;
+        out.push_back(y);
+    }
+    if (kept) {
+        kept->stats = at::empty({p.rows, 4}, in.x.options().dtype(at::kFloat));
+        p.stats = kept->stats.data_ptr<float>();
+        kept->h = p.branch ? h : in.x;
+        if (eight) {
+            const NormEight e(p.rows, p.cols, p.pre, p.post || p.gate);
+            kept->eight = bytes_like(in.x, e.bytes);
+            uint8_t* b = kept->eight.data_ptr<uint8_t>();
+            if (p.pre) { p.h8 = b + e.h.codes; p.h8_scales = b + e.h.scales; }
+            if (p.post || p.gate) { p.u8 = b + e.u.codes; p.u8_scales = b + e.u.scales; }
+        }
+    }
+    check(mxl::check_residual_norm(p), "mx_residual_norm_fwd");
+    check_hip(mxl::launch_residual_norm_fwd(p, stream_of(in.x)), "mx_residual_norm_fwd");
+    return out;
+}
+
+struct MxResidualNormFn : torch::autograd::Function<MxResidualNormFn> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& x, const OptTensor& u, const OptTensor& pre_weight,
+                                                  const OptTensor& pre_bias, const OptTensor& post_weight, const OptTensor& post_bias,
+                                                  const OptTensor& gate, const NormOptions& o, bool eight)
+    {
+        at::AutoDispatchBelowADInplaceOrView guard;
+        const NormInputs in{x, u, pre_weight, pre_bias, post_weight, post_bias, gate};
+        NormKept kept;
+        auto out = norm_forward(in, o, false, eight, &kept);
+        const bool use_u = u && (o.post || gate);                     // the backward pass looks at u itself
+        ctx->set_materialize_grads(false);
+        ctx->save_for_backward({kept.stats, kept.eight, eight || !o.pre ? Tensor() : kept.h, eight || !use_u ? Tensor() : *u,
+                                pre_weight.value_or(Tensor()), post_weight.value_or(Tensor()), post_bias.value_or(Tensor()), gate.value_or(Tensor())});
+        ctx->saved_data["shape"] = x.sizes().vec();
+        auto type = [](const OptTensor& t) { return t ? (int64_t)t->scalar_type() : -1; };
+        ctx->saved_data["types"] = std::vector<int64_t>{(int64_t)x.scalar_type(), type(u), type(pre_weight), type(pre_bias), type(post_weight), type(post_bias), type(gate)};
+        ctx->saved_data["flags"] = std::vector<int64_t>{o.layer, o.pre, o.post, eight};
+        ctx->saved_data["scales"] = std::vector<double>{o.residual_scale, o.branch_scale, o.eps};
+        torch::autograd::variable_list made;
+        for (const Tensor& t : out)
+            if (t.defined()) made.push_back(t);
+        return made;
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        return carried(NORM, [&] { return backward_pass(ctx, grads); });
+    }
+
+    static torch::autograd::variable_list backward_pass(torch::autograd::AutogradContext* ctx, const torch::autograd::variable_list& grads)
+    {
+        const auto keep = ctx->get_saved_variables();
+        const auto shape = ctx->saved_data["shape"].toIntVector(), types = ctx->saved_data["types"].toIntVector(), flags = ctx->saved_data["flags"].toIntVector();
+        const auto scales = ctx->saved_data["scales"].toDoubleVector();
+        const bool branch = types[1] >= 0, pre = flags[1] != 0, post = flags[2] != 0, eight = flags[3] != 0;
+        torch::autograd::variable_list result(9);
+        const Tensor dh_in = branch ? grads[0] : Tensor(), dy_in = pre ? grads[branch ? 1 : 0] : Tensor();
+        if (!dh_in.defined() && !dy_in.defined()) return result;
+        const Tensor& any = dh_in.defined() ? dh_in : dy_in;
+        const Tensor& stats = keep[0];
+        c10::hip::HIPGuard device((c10::DeviceIndex)any.get_device());
+        const int64_t D = shape.back();
+
+        mxl::ResidualNormParams p{};
+        p.cols = D; p.rows = any.numel() / D;
+        p.layer = flags[0] != 0; p.branch = branch; p.pre = pre; p.post = post;
+        p.x_bf16 = (at::ScalarType)types[0] == at::kBFloat16;
+        p.u_bf16 = branch ? (at::ScalarType)types[1] == at::kBFloat16 : p.x_bf16;
+        p.residual_scale = (float)scales[0]; p.branch_scale = (float)scales[1]; p.eps = (float)scales[2];
+        std::vector<Tensor> hold;                                     // dense copies live until the launch is enqueued
+        auto vector_of = [&](const Tensor& t) -> const void* {
+            if (!t.defined()) return nullptr;
+            hold.push_back(t.contiguous());
+            return hold.back().data_ptr();
+        };
+        p.pre_weight = vector_of(keep[4]); p.post_weight = vector_of(keep[5]); p.post_bias = vector_of(keep[6]);
+        for (int i = 2; i < 6; ++i)
+            if (types[i] >= 0) p.param_bf16 = (at::ScalarType)types[i] == at::kBFloat16;
+        if (keep[7].defined()) {
+            const Tensor& gate = keep[7];
+            p.gate_rows = gate.numel() / D;
+            const Rows gr = rows_of(gate.dim() == 2 ? gate : gate.reshape({p.gate_rows, D}), D);
+            hold.push_back(gr.t);
+            p.gate = gr.t.data_ptr(); p.ld_gate = gr.ld; p.gate_bf16 = is_bf16(gate);
+        }
+        // what the forward pass saved may have gone through a program's pack and unpack hooks
+        auto there = [&](const Tensor& t) { return t.get_device() == any.get_device(); };
+        if (stats.scalar_type() != at::kFloat || stats.numel() != 4 * p.rows || !stats.is_contiguous() || !there(stats)) throw Status("mx_residual_norm_bwd", MX_ERR_SHAPE);
+        p.stats = const_cast<float*>(stats.data_ptr<float>());
+        const bool use_u = branch && (post || p.gate);
+        if (eight) {
+            const NormEight e(p.rows, D, pre, use_u);
+            const Tensor& k = keep[1];
+            if (k.scalar_type() != at::kByte || k.numel() != e.bytes || !k.is_contiguous() || !there(k)) throw Status("mx_residual_norm_bwd", MX_ERR_SHAPE);
+            uint8_t* b = k.data_ptr<uint8_t>();
+            if (pre) { p.h8 = b + e.h.codes; p.h8_scales = b + e.h.scales; }
+            if (use_u) { p.u8 = b + e.u.codes; p.u8_scales = b + e.u.scales; }
+        } else {
+            auto matrix = [&](const Tensor& t, bool bf16, int64_t& ld) -> void* {
+                if (t.numel() != p.rows * D || is_bf16(t) != bf16 || !there(t)) throw Status("mx_residual_norm_bwd", MX_ERR_SHAPE);
+                const Rows r = rows_of(t, D);
+                hold.push_back(r.t);
+                ld = r.ld;
+                return r.t.data_ptr();
+            };
+            if (pre) p.h = matrix(keep[2], p.x_bf16, p.ldh);
+            if (use_u) p.u = matrix(keep[3], p.u_bf16, p.ldu);
+        }
+
+        mxl::ResidualNormGrads d{};
+        auto gradient = [&](const Tensor& t, int64_t& ld) -> const void* {
+            if (!t.defined()) return nullptr;
+            const Rows r = rows_of(t, D);
+            hold.push_back(r.t);
+            ld = r.ld;
+            return r.t.data_ptr();
+        };
+        d.dh = gradient(dh_in, d.lddh);
+        d.dy = gradient(dy_in, d.lddy);
+        // results that are asked for; the engine numbers the tensors that the call had
+        int edge = 0;
+        const auto like = any.options();
+        auto wanted = [&](int i, at::IntArrayRef sizes) -> void* {
+            if (types[i] < 0 || !ctx->needs_input_grad(edge++)) return nullptr;
+            result[i] = at::empty(sizes, like.dtype((at::ScalarType)types[i]));
+            return result[i].data_ptr();
+        };
+        d.dx = wanted(0, shape); d.lddx = D;
+        d.du = wanted(1, shape); d.lddu = D;
+        d.dpre_weight = wanted(2, {D}); d.dpre_bias = wanted(3, {D});
+        d.dpost_weight = wanted(4, {D}); d.dpost_bias = wanted(5, {D});
+        d.dgate = wanted(6, keep[7].defined() ? keep[7].sizes() : at::IntArrayRef());
+        if (!dy_in.defined())                                         // nothing of y was used
+            for (int i : {2, 3}) result[i] = Tensor();
+        const size_t bytes = mxl::residual_norm_workspace_bytes(p.rows, D, p.gate ? p.gate_rows : 0);
+        const Tensor workspace = at::empty({(int64_t)bytes}, like.dtype(at::kByte));
+        d.workspace = workspace.data_ptr();
+        check(mxl::check_residual_norm(p), "mx_residual_norm_bwd");
+        check(mxl::check_residual_norm_grads(p, d), "mx_residual_norm_bwd");
+        check_hip(mxl::launch_residual_norm_bwd(p, d, stream_of(any)), "mx_residual_norm_bwd");
+        return result;
+    }
+};
+
+bool records(std::initializer_list<const OptTensor*> tensors)
+{
+    if (!at::GradMode::is_enabled()) return false;
+    for (const OptTensor* t : tensors)
+        if (*t && (*t)->requires_grad()) return true;
+    return false;
+}
+
+// A call recorded into a graph whose input already belongs to an autograd graph of another stream (a leaf of an eager graph
+// that is still alive, say): its backward pass would run that input's node on the other stream in the middle of the capture,
+// which ends the process.  Refused here.
+void check_recorded(const char* what, const Tensor& on, std::initializer_list<const OptTensor*> tensors)
+{
+    const auto stream = c10::hip::getCurrentHIPStream(on.get_device());
+    if (!is_capturing(stream.stream())) return;
+    for (const OptTensor* t : tensors) {
+        if (!*t || !(*t)->requires_grad()) continue;
+        const auto node = (*t)->grad_fn() ? (*t)->grad_fn() : torch::autograd::impl::try_get_grad_accumulator(**t);
+        if (!node) continue;
+        const auto theirs = node->stream();
+        TORCH_CHECK(!theirs || *theirs == stream.unwrap(), what, ": an input of this recorded call belongs to an autograd graph that was made on another "
+                    "stream and is still alive; let that graph go first, or record the call with detached inputs");
+    }
+}
+
+// (h, y), or packed (h, codes, scales); None for what there is not.
+std::vector<OptTensor> residual_norm(const Tensor& x, const OptTensor& u, const OptTensor& pre_weight, const OptTensor& pre_bias, const OptTensor& post_weight,
+                                     const OptTensor& post_bias, const OptTensor& gate, bool layer, bool pre, bool post, double residual_scale,
+                                     double branch_scale, double eps, bool eight, bool packed, int scale_mode)
+{
+    const NormInputs in{x, u, pre_weight, pre_bias, post_weight, post_bias, gate};
+    const NormOptions o{layer, pre, post, floor_of(scale_mode, "mx_residual_norm_fwd"), (float)residual_scale, (float)branch_scale, (float)eps};
+    check_norm_call(in, o, packed);
+    c10::hip::HIPGuard device((c10::DeviceIndex)x.get_device());
+    const OptTensor xo = x;
+    const bool grad = records({&xo, &u, &pre_weight, &pre_bias, &post_weight, &post_bias, &gate});
+    TORCH_CHECK_VALUE(!grad || !packed, "packed codes carry no gradient: call it under torch.no_grad()");
+    if (grad) check_recorded(NORM, x, {&xo, &u, &pre_weight, &pre_bias, &post_weight, &post_bias, &gate});
+    std::vector<OptTensor> r{u ? OptTensor() : xo};
+    torch::autograd::variable_list out;
+    if (grad) {
+        out = MxResidualNormFn::apply(x, u, pre_weight, pre_bias, post_weight, post_bias, gate, o, eight);
+    } else {
+        at::AutoDispatchBelowADInplaceOrView guard;
+        out = norm_forward(in, o, packed, false, nullptr);
+        if (!u) out.erase(out.begin());
+    }
+    size_t i = 0;
+    if (u) r[0] = out[i++];
+    if (!pre) r.push_back(OptTensor());
+    for (; i < out.size(); ++i) r.push_back(out[i]);
+    return r;
+}
+
+constexpr const char* ACT = "activation";
+
+mxl::ActivationParams act_params(const Rows& p, bool bf16, bool silu, bool gated)
+{
+    mxl::ActivationParams a{};
+    a.p = p.t.data_ptr(); a.ldp = p.ld; a.bf16 = bf16;
+    a.rows = p.rows; a.cols = gated ? p.cols / 2 : p.cols;
+    a.silu = silu; a.gated = gated;
+    return a;
+}
+
+// Outputs {a}, packed {codes, scales}; kept8: receives the checkpoint of p.
+torch::autograd::variable_list act_forward(const Tensor& p, bool silu, bool gated, bool packed, bool floor_mode, Tensor* kept8)
+{
+    const Rows r = rows_of(p, p.size(-1));
+    mxl::ActivationParams a = act_params(r, is_bf16(p), silu, gated);
+    torch::autograd::variable_list out;
+    a.floor_mode = floor_mode;
+    if (packed) {
+        out = {at::empty({a.rows, a.cols / 2}, p.options().dtype(at::kByte)), at::empty({a.rows, a.cols / 32}, p.options().dtype(at::kByte))};
+        a.a_codes = out[0].data_ptr<uint8_t>(); a.a_scales = out[1].data_ptr<uint8_t>();
+    } else {
+        out = {at::empty(with_last(p.sizes(), a.cols), p.options())};
+        a.a = out[0].data_ptr(); a.lda = a.cols;
+    }
+    if (kept8) {
+        Carver c;
+        const Eight e = carve8(c, a.rows * (gated ? 2 : 1), a.cols);
+        *kept8 = bytes_like(p, c.used);
+        a.p8 = kept8->data_ptr<uint8_t>() + e.codes; a.p8_scales = kept8->data_ptr<uint8_t>() + e.scales;
+    }
+    check(mxl::check_activation(a, false), "mx_activation_fwd");
+    check_hip(mxl::launch_activation_fwd(a, stream_of(p)), "mx_activation_fwd");
+    return out;
+}
+
+struct MxActivationFn : torch::autograd::Function<MxActivationFn> {
+    static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& p, bool silu, bool gated, bool eight)
+    {
+        at::AutoDispatchBelowADInplaceOrView guard;
+        Tensor kept;
+        const Tensor a = act_forward(p, silu, gated, false, false, eight ? &kept : nullptr)[0];
+        ctx->save_for_backward({eight ? kept : p});
+        ctx->saved_data["shape"] = p.sizes().vec();
+        ctx->saved_data["flags"] = std::vector<int64_t>{silu, gated, eight, (int64_t)p.scalar_type()};
+        return a;
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        return carried(ACT, [&] { return backward_pass(ctx, grads[0]); });
+    }
+
+    static torch::autograd::variable_list backward_pass(torch::autograd::AutogradContext* ctx, const Tensor& da)
+    {
+        const Tensor kept = ctx->get_saved_variables()[0];
+        const auto shape = ctx->saved_data["shape"].toIntVector(), flags = ctx->saved_data["flags"].toIntVector();
+        const bool gated = flags[1] != 0, eight = flags[2] != 0;
+        c10::hip::HIPGuard device((c10::DeviceIndex)da.get_device());
+        mxl::ActivationParams a{};
+        a.silu = flags[0] != 0; a.gated = gated; a.bf16 = (at::ScalarType)flags[3] == at::kBFloat16;
+        a.cols = gated ? shape.back() / 2 : shape.back();
+        const Rows d = rows_of(da, a.cols);
+        a.rows = d.rows;
+        a.a = d.t.data_ptr(); a.lda = d.ld;
+        const Tensor dp = at::empty(shape, da.options());
+        a.dp = dp.data_ptr(); a.lddp = shape.back();
+        Rows p{};
+        // what the forward pass saved may have gone through a program's pack and unpack hooks
+        if (kept.get_device() != da.get_device()) throw Status("mx_activation_bwd", MX_ERR_SHAPE);
+        if (eight) {
+            Carver c;
+            const Eight e = carve8(c, a.rows * (gated ? 2 : 1), a.cols);
+            if (kept.scalar_type() != at::kByte || kept.numel() != c.used || !kept.is_contiguous()) throw Status("mx_activation_bwd", MX_ERR_SHAPE);
+            a.p8 = kept.data_ptr<uint8_t>() + e.codes; a.p8_scales = kept.data_ptr<uint8_t>() + e.scales;
+        } else {
+            if (kept.sizes() != at::IntArrayRef(shape) || is_bf16(kept) != a.bf16) throw Status("mx_activation_bwd", MX_ERR_SHAPE);
+            p = rows_of(kept, shape.back());
+            a.p = p.t.data_ptr(); a.ldp = p.ld;
+        }
+        check(mxl::check_activation(a, true), "mx_activation_bwd");
+        check_hip(mxl::launch_activation_bwd(a, stream_of(da)), "mx_activation_bwd");
+        return {dp, Tensor(), Tensor(), Tensor()};
+    }
+};
+
+std::vector<Tensor> activation(const Tensor& p, bool silu, bool gated, bool eight, bool packed, int scale_mode)
+{
+    const bool floor_mode = floor_of(scale_mode, "mx_activation_fwd");
+    no_trace(ACT);
+    const OptTensor po = p;
+    no_tangent(ACT, {&po});
+    (void)is_bf16(p);
+    TORCH_CHECK_VALUE(p.dim() >= 1 && (!gated || p.size(-1) % 2 == 0), "a gated activation takes two halves of one length, got ", p.sizes());
+    if (p.numel() == 0) throw Status("mx_activation_fwd", MX_ERR_SHAPE);
+    {
+        const Rows r = rows_of(p, p.size(-1));
+        const mxl::ActivationParams a = act_params(r, is_bf16(p), silu, gated);
+        check(mxl::check_activation(a, false), "mx_activation_fwd");
+        if (packed && a.cols % 32 != 0) throw Status("mx_activation_fwd", MX_ERR_SHAPE);
+    }
+    TORCH_CHECK(p.is_cuda(), ACT, " runs on the GPU");
+    c10::hip::HIPGuard device((c10::DeviceIndex)p.get_device());
+    if (records({&po})) {
+        TORCH_CHECK_VALUE(!packed, "packed codes carry no gradient: call it under torch.no_grad()");
+        check_recorded(ACT, p, {&po});
+        return {MxActivationFn::apply(p, silu, gated, eight)};
+    }
+    at::AutoDispatchBelowADInplaceOrView guard;
+    return act_forward(p, silu, gated, packed, floor_mode, nullptr);
+}
+
 // ---- QRampingAdamW: one call per parameter group ----
 
 // A tensor of an optimizer state dict.
@@ -609,6 +1168,10 @@ PYBIND11_MODULE(_mx_torch, m)
         mx_error_class = cls.release().ptr();
     });
     m.def("linear", &linear, py::call_guard<py::gil_scoped_release>());
+    m.def("residual_norm", &residual_norm, py::call_guard<py::gil_scoped_release>());
+    m.def("activation", &activation, py::call_guard<py::gil_scoped_release>());
+    m.def("checkpoint_pack", &checkpoint_pack, py::call_guard<py::gil_scoped_release>());
+    m.def("checkpoint_unpack", &checkpoint_unpack, py::call_guard<py::gil_scoped_release>());
     m.def("linear_fits_one_launch", &mxl::linear_fits_one_launch);           // the rules, for tests
     m.def("gemm_kernel_name", &mxl::gemm_kernel_name);
     m.def("tile_workgroups", &mxl::tile_workgroups);
