@@ -421,8 +421,8 @@ int mx_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, int64_t ro
  *   gate          device, gate_dtype, gate_rows rows with stride ld_gate, or NULL; gate_rows divides rows, and each gate
  *                 row is that of rows / gate_rows consecutive rows (1: one for all; the number of sequences; rows)
  *   h8, h8_scales, u8, u8_scales   device out, each pair or NULL: mx_checkpoint_pack of h and of u
- *   stats         device out, FP32 [rows][4], 16-byte aligned, or NULL: mean and r of u, mean and r of h (0 where there is
- *                 no such norm, or no mean), for the backward pass
+ *   stats         device out, FP32 [rows][4], 16-byte aligned, or NULL: mean and r of u, mean and r of h, for the backward
+ *                 pass (the mean 0 for MX_NORM_RMS; unspecified where there is no such norm)
  * 1 <= cols <= 16384, rows * cols < 2^35; eps at least 2^-126 (MX_ERR_MODE); pointers at the alignment of their elements
  * unless stated.  At least one of h and y is asked for.
  */

@@ -9,8 +9,8 @@ import tempfile
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libmxfp4_hip.so")
-SOURCES = ["mx_api.hip", "mx_quant.hip", "mx_gemm.hip", "mx_optim.hip", "mx_norm.hip", "mx_act.hip"]
-HEADERS = ["mx_device.hpp", "mx_block.hpp", "mx_launch.hpp", os.path.join("..", "..", "include", "mxfp4.h")]
+SOURCES = ["mx_api.hip", "mx_quant.hip", "mx_gemm.hip", "mx_optim.hip", "mx_norm.hip", "mx_norm_bwd_rms.hip", "mx_norm_bwd_layer.hip", "mx_act.hip"]
+HEADERS = ["mx_device.hpp", "mx_block.hpp", "mx_norm.hpp", "mx_norm_bwd.hpp", "mx_launch.hpp", os.path.join("..", "..", "include", "mxfp4.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

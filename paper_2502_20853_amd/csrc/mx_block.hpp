@@ -253,7 +253,7 @@ struct Team {
     // Consecutive sums use the two halves of the scratch in turn: a wave writes a half again only behind the barrier
     // of the sum between, which every wave reaches after its last read of that half.
     template <int N>
-    __device__ __forceinline__ void sum(float (&v)[N])
+    __device__ __forceinline__ void sum(float* v)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = wave_part_sum(v[i], lanes);

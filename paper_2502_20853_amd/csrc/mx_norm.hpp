@@ -1,0 +1,332 @@
+// Gated residual with the norms on both sides of a block, and its backward pass: what their launches share.
+//     v = post ? n(u; post_weight, post_bias) : u
+//     h = rho x + sigma g . v                       stored in the stream's type
+//     y = n(h; pre_weight, pre_bias)                of the stored h; in the branch's type, or as MXFP4 codes
+// with n(a; w, b) = a r w, r = (mean a^2 + eps)^-1/2 (RMS), or (a - mu) r w + b, r = (var a + eps)^-1/2 (layer).
+// Backward, with a^ the normalised input (a - mu) r:
+//     b = dy pre_weight;        dh = dh_out + r_h (b - [mean b] - h^ mean(b h^));     dx = rho dh
+//     dv = sigma g . dh;        c = dv post_weight;     du = r_u (c - [mean c] - u^ mean(c u^))
+//     d_pre_weight = sum dy h^, d_pre_bias = sum dy, d_post_weight = sum dv u^, d_post_bias = sum dv,
+//     d_gate = sum sigma dh . v        ([...]: layer only; the sums run over rows, for the gate over its rows)
+//
+// Both passes are bound by memory (8 to 12 bytes an element in bf16 against 40 to 60 vector instructions for eight of
+// them), so a row is read once: a team of lanes holds it in registers, V vectors of eight elements a lane, through both norms.
+#pragma once
+#include "mx_block.hpp"
+
+#include <algorithm>
+
+namespace mxl {
+
+using namespace mxb;
+
+struct NormArgs {
+    const void* x;
+    const void* u;
+    void* h;
+    void* y;
+    const void* pre_weight;
+    const void* pre_bias;
+    const void* post_weight;
+    const void* post_bias;
+    const void* gate;
+    uint8_t* y_codes;
+    uint8_t* y_scales;
+    uint8_t* h8;
+    uint8_t* h8_scales;
+    uint8_t* u8;
+    uint8_t* u8_scales;
+    float4* stats;
+    int64_t rows, ldx, ldu, ldh, ldy, ld_gate, gate_run;      // gate_run: rows of the stream that share a gate row
+    int64_t teams, team_rows, row_step;                       // teams of the launch, the most rows that one has, from one to the next
+    uint32_t cols, pitch8, lanes;
+    float inv_cols, rho, sigma, eps;
+    bool layer, post, param_bf16, gate_bf16, gate_by_row, floor_mode;
+};
+
+struct NormGradArgs {
+    NormArgs f;
+    const void* dh;
+    const void* dy;
+    void* dx;
+    void* du;
+    int64_t lddh, lddy, lddx, lddu;
+    float* partials;          // [SUMS][workgroups][cols]
+    float* gate_partials;     // [gate rows x pieces][cols], or [workgroups][cols] for a gate of one row
+    void* dgate;              // where whole gate rows belong to one team
+    int64_t gate_rows, pieces;                                // pieces 0: teams own whole gate rows
+    bool want_gate;
+};
+
+enum NormSum { PRE_WEIGHT, POST_WEIGHT, GATE_SUM, PRE_BIAS, POST_BIAS, SUMS };
+enum NormParam { P_PRE_WEIGHT, P_POST_WEIGHT, P_GATE, P_PRE_BIAS, P_POST_BIAS, PARAMS };
+
+constexpr uint32_t UNITS = 256;                          // compute units
+constexpr uint32_t NORM_THREADS = 512;                   // the largest workgroup: rows of 16384 at four vectors a lane
+constexpr size_t NORM_LDS_MAX = 160 * 1024 - sizeof(TeamScratch);
+
+// How many elements the row has from `col` on (not positive: none).
+__device__ __forceinline__ int left(uint32_t cols, uint32_t col) { return (int)cols - (int)col; }
+
+// The parameters in LDS: for each eight columns the eight values of every parameter one behind the other, and four words
+// more, so that the 16-byte reads of neighbouring lanes fall into different banks.  A lane needs one address for all of them.
+template <bool POST, bool GATE, bool LAYER, bool BACKWARD>
+struct ParamLds {
+    static constexpr uint32_t GATE_SLOT = 1 + POST, PRE_BIAS_SLOT = GATE_SLOT + GATE, POST_BIAS_SLOT = PRE_BIAS_SLOT + (LAYER && !BACKWARD);
+    static constexpr uint32_t STRIDE = (POST_BIAS_SLOT + (LAYER && POST)) * 8 + 4;      // words from one eight columns to the next
+    static constexpr uint32_t GATE_STRIDE = 12;                          // the same for a gate row of a team's own
+    static constexpr uint32_t slot(NormParam p)
+    {
+        return p == P_PRE_WEIGHT ? 0 : p == P_POST_WEIGHT ? 1 : p == P_GATE ? GATE_SLOT : p == P_PRE_BIAS ? PRE_BIAS_SLOT : POST_BIAS_SLOT;
+    }
+    static __device__ __forceinline__ void put(float* lds, NormParam p, uint32_t vector, const F8& f) { put(lds + vector * STRIDE + slot(p) * 8, f); }
+    static __device__ __forceinline__ F8 get(const float* lds, NormParam p, uint32_t vector) { return get(lds + vector * STRIDE + slot(p) * 8); }
+    static __device__ __forceinline__ void put(float* at, const F8& f)
+    {
+        float4* to = reinterpret_cast<float4*>(at);
+        to[0] = make_float4(f.v[0], f.v[1], f.v[2], f.v[3]);
+        to[1] = make_float4(f.v[4], f.v[5], f.v[6], f.v[7]);
+    }
+    static __device__ __forceinline__ F8 get(const float* at)
+    {
+        const float4* from = reinterpret_cast<const float4*>(at);
+        const float4 lo = from[0], hi = from[1];
+        return F8{{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}};
+    }
+};
+
+// A parameter's eight values from `col` on, from memory.
+template <bool TAIL>
+__device__ __forceinline__ F8 norm_param(const NormArgs& g, int which, uint32_t col)
+{
+    const int n = left(g.cols, col);
+    switch (which) {
+        case P_PRE_WEIGHT:  return param8<TAIL>(g.pre_weight, g.param_bf16, col, n, 1.0f);
+        case P_POST_WEIGHT: return param8<TAIL>(g.post_weight, g.param_bf16, col, n, 1.0f);
+        case P_PRE_BIAS:    return param8<TAIL>(g.pre_bias, g.param_bf16, col, n, 0.0f);
+        case P_POST_BIAS:   return param8<TAIL>(g.post_bias, g.param_bf16, col, n, 0.0f);
+        default:            return param8<TAIL>(g.gate, g.gate_bf16, col, n, 1.0f);
+    }
+}
+
+// ---- a team's rows of a matrix ---------------------------------------------------------------------
+// ANY: rows of any length and alignment, by address.  Else (a length of whole vectors, 16-byte rows) through a buffer
+// descriptor that starts at a row which is the same for the whole workgroup: the descriptor moves on by scalar instructions, a
+// lane's offset from there never changes, and a lane without work has one beyond the descriptor's end, where the hardware
+// returns zero and drops stores.  That saves the address arithmetic and its registers, and every branch.
+// A matrix that there is not (null) reads as zero and takes no stores.
+constexpr uint32_t OFF_END = 0x80000000u;                // beyond the end of every descriptor
+constexpr int64_t OFF_MAX = 0x7FFFFFF0;                  // what one covers: a workgroup's rows have to fit
+
+typedef uint32_t u4_vec __attribute__((ext_vector_type(4)));
+typedef uint32_t u2_vec __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const void* base, int64_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + bytes, (short)0, base == nullptr ? 0 : (int)OFF_MAX, 0x00020000);
+}
+
+constexpr int NT = 2;                                    // the nontemporal bit: what is loaded is not read again soon
+
+__device__ __forceinline__ RawBf16 buffer_load_raw(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t step, uint16_t)
+{
+    const u4_vec a = __builtin_amdgcn_raw_buffer_load_b128(r, off, step, NT);
+    return RawBf16{{a.x, a.y, a.z, a.w}};
+}
+__device__ __forceinline__ F8 buffer_load_raw(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t step, float)
+{
+    const u4_vec a = __builtin_amdgcn_raw_buffer_load_b128(r, off, step, NT), b = __builtin_amdgcn_raw_buffer_load_b128(r, off + 16u, step, NT);
+    return F8{{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+               __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)}};
+}
+// The step is added to the lane's offset: a 16-byte store with its offset in a scalar register reads its data late enough that an
+// instruction right behind it, which the compiler takes to be safe there, has overwritten it (the first word of 16 lanes at a
+// time); without one the compiler keeps the distance.
+__device__ __forceinline__ void buffer_store_raw(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t step, const RawBf16& v)
+{
+    __builtin_amdgcn_raw_buffer_store_b128(u4_vec{v.w[0], v.w[1], v.w[2], v.w[3]}, r, off + step, 0, 0);
+}
+__device__ __forceinline__ void buffer_store_raw(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t step, const F8& v)
+{
+    const float* f = v.v;
+    __builtin_amdgcn_raw_buffer_store_b128(u4_vec{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])}, r, off + step, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(u4_vec{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])}, r, off + step + 16u, 0, 0);
+}
+
+// Where a lane of a team is: the workgroup's row `first`, and the team's so many rows behind it; both move on together.
+struct Place {
+    int64_t first;
+    uint32_t behind;
+    uint32_t col0, step;     // the lane's first column, columns from one of its vectors to the next
+    uint32_t cols, pitch8;
+    uint32_t live;           // whether the team has a row
+    __device__ __forceinline__ int64_t row() const { return first + behind; }
+    __device__ __forceinline__ uint32_t col(int v) const { return col0 + v * step; }
+    __device__ __forceinline__ int left(int v) const { return live != 0 ? (int)cols - (int)col(v) : 0; }
+    // Only the last of a lane's vectors can lie behind the row's end.
+    template <int V> __device__ __forceinline__ bool in(int v, uint32_t end) const { return live != 0 && (v < V - 1 || col(v) < end); }
+};
+
+template <bool ANY, int V, typename T>
+__device__ __forceinline__ Raw<T> load_vec(const void* base, int64_t ld, const Place& at, int v)
+{
+    if constexpr (ANY) return load_raw<true>(static_cast<const T*>(base) + at.row() * ld + at.col(v), base == nullptr ? 0 : at.left(v));
+    const uint32_t off = (at.behind * (uint32_t)ld + at.col0) * sizeof(T);
+    return buffer_load_raw(descriptor(base, at.first * ld * (int64_t)sizeof(T)), at.in<V>(v, at.cols) ? off : OFF_END, v * at.step * sizeof(T), T{});
+}
+
+template <bool ANY, int V, typename T>
+__device__ __forceinline__ void store_vec(void* base, int64_t ld, const Place& at, int v, const F8& f)
+{
+    Raw<T> raw;
+    narrow(f, raw);
+    if constexpr (ANY) {
+        store_raw<true>(static_cast<T*>(base) + at.row() * ld + at.col(v), raw, base == nullptr ? 0 : at.left(v));
+        return;
+    }
+    const uint32_t off = (at.behind * (uint32_t)ld + at.col0) * sizeof(T);
+    buffer_store_raw(descriptor(base, at.first * ld * (int64_t)sizeof(T)), at.in<V>(v, at.cols) ? off : OFF_END, v * at.step * sizeof(T), raw);
+}
+
+// 8-bit codes and scale bytes; their rows are whole groups, so they always go through descriptors.
+template <int V>
+__device__ __forceinline__ void store_codes8(uint8_t* codes, uint8_t* scales, const Place& at, int v, const F8& f)
+{
+    uint32_t byte;
+    const Codes8 c = pack8(f, byte);
+    const bool in = at.in<V>(v, at.pitch8);
+    const uint32_t groups = at.pitch8 >> 5;
+    __builtin_amdgcn_raw_buffer_store_b64(u2_vec{c.w[0], c.w[1]}, descriptor(codes, at.first * at.pitch8), in ? at.behind * at.pitch8 + at.col0 : OFF_END, v * at.step, 0);
+    __builtin_amdgcn_raw_buffer_store_b8((uint8_t)byte, descriptor(scales, at.first * groups),
+                                         in && (at.col0 & 31u) == 0 ? at.behind * groups + (at.col0 >> 5) : OFF_END, v * at.step >> 5, 0);
+}
+
+template <int V>
+__device__ __forceinline__ Codes8 load_codes8(const uint8_t* codes, const uint8_t* scales, const Place& at, int v, uint32_t& byte)
+{
+    const bool in = at.in<V>(v, at.pitch8);
+    const uint32_t groups = at.pitch8 >> 5;
+    const u2_vec c = __builtin_amdgcn_raw_buffer_load_b64(descriptor(codes, at.first * at.pitch8), in ? at.behind * at.pitch8 + at.col0 : OFF_END, v * at.step, NT);
+    byte = __builtin_amdgcn_raw_buffer_load_b8(descriptor(scales, at.first * groups), in ? at.behind * groups + (at.col0 >> 5) : OFF_END, v * at.step >> 5, 0);
+    return Codes8{{c.x, c.y}};
+}
+
+// The value is used from here on as it stands in its registers: what was computed from it before is computed again, not kept.
+__device__ __forceinline__ void renew(RawBf16& r) { asm volatile("" : "+v"(r.w[0]), "+v"(r.w[1]), "+v"(r.w[2]), "+v"(r.w[3])); }
+__device__ __forceinline__ void renew(F8& r)
+{
+    asm volatile("" : "+v"(r.v[0]), "+v"(r.v[1]), "+v"(r.v[2]), "+v"(r.v[3]), "+v"(r.v[4]), "+v"(r.v[5]), "+v"(r.v[6]), "+v"(r.v[7]));
+}
+__device__ __forceinline__ void renew(Codes8& c) { asm volatile("" : "+v"(c.w[0]), "+v"(c.w[1])); }
+
+// What was loaded before is loaded again behind this, not kept: registers are short, and parameters near.
+__device__ __forceinline__ void forget() { asm volatile("" ::: "memory"); }
+
+// Lanes and vectors a lane of a team.
+struct TeamShape {
+    uint32_t lanes;
+    int v;
+};
+
+inline uint32_t lanes_for(int64_t vectors)
+{
+    for (uint32_t l = 8; l < 64; l *= 2)
+        if (vectors <= l) return l;
+    return (uint32_t)((vectors + 63) / 64 * 64);
+}
+
+// Teams of a workgroup, raised to whole waves.
+inline uint32_t whole_waves(uint32_t teams, uint32_t lanes)
+{
+    const uint32_t per = lanes < 64 ? 64 / lanes : 1;
+    return (teams + per - 1) / per * per;
+}
+
+inline NormArgs norm_args(const ResidualNormParams& p, const TeamShape& shape)
+{
+    NormArgs g{};
+    g.x = p.x; g.u = p.u; g.h = p.h; g.y = p.y;
+    g.pre_weight = p.pre_weight; g.pre_bias = p.pre_bias; g.post_weight = p.post_weight; g.post_bias = p.post_bias; g.gate = p.gate;
+    g.y_codes = p.y_codes; g.y_scales = p.y_scales;
+    g.h8 = p.h8; g.h8_scales = p.h8_scales; g.u8 = p.u8; g.u8_scales = p.u8_scales;
+    g.stats = reinterpret_cast<float4*>(p.stats);
+    g.rows = p.rows; g.ldx = p.ldx; g.ldu = p.ldu; g.ldh = p.ldh; g.ldy = p.ldy; g.ld_gate = p.ld_gate;
+    g.gate_run = p.gate != nullptr && p.gate_rows > 0 ? p.rows / p.gate_rows : p.rows;
+    g.gate_by_row = p.gate != nullptr && p.gate_rows > 1;
+    g.cols = (uint32_t)p.cols; g.pitch8 = (uint32_t)((p.cols + 31) / 32 * 32);
+    g.lanes = shape.lanes;
+    g.inv_cols = (float)(1.0 / (double)p.cols);
+    g.rho = p.residual_scale; g.sigma = p.branch_scale; g.eps = p.eps;
+    g.layer = p.layer; g.post = p.post;
+    g.param_bf16 = p.param_bf16; g.gate_bf16 = p.gate_bf16; g.floor_mode = p.floor_mode;
+    return g;
+}
+
+// Calls f with the element types of the stream and the branch.
+template <typename F>
+void by_types(bool x_bf16, bool u_bf16, F&& f)
+{
+    if (x_bf16) f(uint16_t{}, uint16_t{});
+    else if (u_bf16) f(float{}, uint16_t{});
+    else f(float{}, float{});
+}
+
+// Calls f with a truth value, with what a kernel is compiled for (post-norm, gate, rows of any kind), or with a number of
+// vectors, as types.
+template <typename F>
+void by_flag(bool a, F&& f) { a ? f(std::true_type{}) : f(std::false_type{}); }
+template <typename F>
+void by_kind(bool any, bool post, bool gate, F&& f)
+{
+    using Y = std::true_type;
+    using N = std::false_type;
+    // rows of any length and alignment have one kernel for all kinds
+    if (any)       f(Y{}, Y{}, Y{});
+    else if (post) gate ? f(Y{}, Y{}, N{}) : f(Y{}, N{}, N{});
+    else           gate ? f(N{}, Y{}, N{}) : f(N{}, N{}, N{});
+}
+template <bool THREE, typename F>
+void by_vectors(int v, F&& f)
+{
+    if (v == 1)      f(std::integral_constant<int, 1>{});
+    else if (v == 2) f(std::integral_constant<int, 2>{});
+    else if (v == 4) f(std::integral_constant<int, 4>{});
+    else if constexpr (THREE) f(std::integral_constant<int, 3>{});
+}
+
+// Whether a matrix's rows go through descriptors: `rows` of them from a workgroup's first one on.
+inline bool by_descriptor(const void* p, bool bf16, int64_t ld, int64_t rows)
+{
+    const int64_t bytes = bf16 ? 2 : 4;
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * bytes % 16 == 0 && rows <= OFF_MAX / bytes / std::max<int64_t>(1, ld) - 1;
+}
+
+// Bytes of LDS that the parameters of a kernel take (the ParamLds of its kind), and gate rows of the teams' own.
+inline size_t param_bytes(const TeamShape& s, bool any, bool post, bool gate, bool layer, bool backward, uint32_t own_gates)
+{
+    size_t words = 0;
+    by_kind(any, post, gate, [&](auto p, auto g, auto) {
+        by_flag(layer, [&](auto l) {
+            by_flag(backward, [&](auto b) { words = ParamLds<decltype(p)::value, decltype(g)::value, decltype(l)::value, decltype(b)::value>::STRIDE; });
+        });
+    });
+    return (words + (size_t)own_gates * 12) * s.lanes * s.v * sizeof(float);
+}
+
+// Starts a kernel with `lds` bytes, asking for more than a kernel may have by itself where need be.
+template <typename K, typename A>
+hipError_t start_norm(K kernel, uint32_t grid, uint32_t threads, size_t lds, hipStream_t st, const A& args)
+{
+    if (lds > 65536 - sizeof(TeamScratch)) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<grid, threads, lds, st>>>(args);
+    return hipGetLastError();
+}
+
+// The backward kernels by norm (a file each).
+hipError_t launch_norm_bwd_rms(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, uint32_t grid, uint32_t threads, size_t lds, hipStream_t st);
+hipError_t launch_norm_bwd_layer(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, uint32_t grid, uint32_t threads, size_t lds, hipStream_t st);
+
+}  // namespace mxl

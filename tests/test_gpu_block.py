@@ -122,6 +122,31 @@ def test_residual_norm_widths(mx, d, n):
         run_case(mx, n, d, *types, layer, True, 1, ckpt, 10 + i)
 
 
+@pytest.mark.parametrize("d", [33, 1001, 4099, 12001])
+def test_odd_rows_of_every_kind(mx, d):
+    """Rows of no whole vectors, with and without a post-norm, a gate, gate rows, 8-bit checkpoints."""
+    i = 0
+    for layer in (False, True):
+        for post in (False, True):
+            for gates in (0, 1, 3):
+                for ckpt in (False, True):
+                    i += 1
+                    print("odd", d, layer, post, gates, ckpt, flush=True)
+                    run_case(mx, 9, d, *[(BF, BF, BF), (F32, BF, F32), (F32, F32, F32)][i % 3], layer, post, gates, ckpt, 40 + i)
+
+
+@pytest.mark.parametrize("d", [768, 2048, 4096, 8192, 16384])
+def test_whole_rows_of_every_kind(mx, d):
+    i = 0
+    for layer in (False, True):
+        for post in (False, True):
+            for gates in (0, 1, 3):
+                for ckpt in (False, True):
+                    i += 1
+                    print("whole", d, layer, post, gates, ckpt, flush=True)
+                    run_case(mx, 9, d, *[(BF, BF, BF), (F32, BF, F32), (F32, F32, F32)][i % 3], layer, post, gates, ckpt, 70 + i)
+
+
 @pytest.mark.parametrize("n,d,gates", [(12, 40, 12), (12, 40, 4), (600, 72, 2), (600, 72, 300), (1970, 192, 10), (4096, 64, 4096), (1, 64, 1),
                                        (1200, 33, 600), (5000, 520, 25), (3000, 1100, 1500)])
 def test_gate_rows(mx, n, d, gates):
