@@ -105,7 +105,8 @@ __device__ __forceinline__ void store_raw(uint16_t* p, const RawBf16& r, int n)
             v.x = r.w[0]; v.y = r.w[1];
             *reinterpret_cast<u2_any*>(p) = v;
         }
-        const uint32_t a = n & 4 ? r.w[2] : r.w[0], b = n & 4 ? r.w[3] : r.w[1];
+        const uint32_t w0 = r.w[0], w1 = r.w[1], w2 = r.w[2], w3 = r.w[3];         // by value: no indexed registers
+        const uint32_t a = n & 4 ? w2 : w0, b = n & 4 ? w3 : w1;
         if (n & 2) *reinterpret_cast<u1_any*>(p + (n & 4)) = a;
         if (n & 1) p[n & 6] = (uint16_t)(n & 2 ? b : a);
     }
