@@ -54,6 +54,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
     extern __shared__ float lds[];                                       // the parameters, where a lane has two or three vectors
     __shared__ TeamScratch scratch;
     using Params = ParamLds<POST, GATE, true, false>;
+    const uint32_t stride = g.layer ? Params::STRIDE : ParamLds<POST, GATE, false, false>::STRIDE;      // the biases come last
     const uint32_t team_in_block = threadIdx.x / g.lanes, lane = threadIdx.x % g.lanes;
     const uint32_t teams = blockDim.x / g.lanes;
     Team team{g.lanes, team_in_block * (g.lanes >> 6), &scratch};
@@ -80,16 +81,23 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
     F8 held[PARAMS];
     auto each_param = [&](auto&& f) {
         f(P_PRE_WEIGHT);
-        f(P_PRE_BIAS);
+        if (g.layer) f(P_PRE_BIAS);
         if (POST) f(P_POST_WEIGHT);
-        if (POST) f(P_POST_BIAS);
+        if (POST && g.layer) f(P_POST_BIAS);
         if (GATE && !gate_by_row) f(P_GATE);
     };
     if constexpr (V == 1) {
         each_param([&](NormParam which) { held[which] = norm_param<ANY>(g, which, at.col0); });
     } else if constexpr (V < 4) {
         each_param([&](NormParam which) {
-            for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x) Params::put(lds, which, c, norm_param<ANY>(g, which, c * 8));
+            for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x) Params::put(lds, stride, which, c, norm_param<ANY>(g, which, c * 8));
+        });
+        __syncthreads();
+    } else {
+        each_param([&](NormParam which) {
+            if (g.plane[which] == ParamPlanes::NO_PLANE) return;
+            for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x)
+                ParamPlanes::put(lds, g.plane[which], vectors, c, param_is_bf16(g, which), norm_param<ANY>(g, which, c * 8));
         });
         __syncthreads();
     }
@@ -99,7 +107,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
         gate_row = at.row() / g.gate_run;
         in_run = at.row() - gate_row * g.gate_run;
     }
-    float* own_gate = lds + vectors * Params::STRIDE + team_in_block * vectors * Params::GATE_STRIDE;     // a lane reads what it wrote
+    float* own_gate = lds + vectors * stride + team_in_block * vectors * Params::GATE_STRIDE;     // a lane reads what it wrote
     auto gate_of_row = [&](int v) { return param8<ANY>(g.gate, g.gate_bf16, gate_row * g.ld_gate + at.col(v), at.left(v), 0.0f); };
     auto take_gate = [&]() {
         if constexpr (V == 1) held[P_GATE] = gate_of_row(0);
@@ -113,9 +121,11 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
         if constexpr (V == 1) return held[which];
         else if constexpr (V < 4) {
             if (which == P_GATE && gate_by_row) return Params::get(own_gate + (lane + v * g.lanes) * Params::GATE_STRIDE);
-            return Params::get(lds, which, lane + v * g.lanes);
+            return Params::get(lds, stride, which, lane + v * g.lanes);
         } else {
-            return which == P_GATE && gate_by_row ? gate_of_row(v) : norm_param<ANY>(g, which, at.col(v));
+            if (which == P_GATE && gate_by_row) return gate_of_row(v);
+            if (g.plane[which] != ParamPlanes::NO_PLANE) return ParamPlanes::get(lds, g.plane[which], vectors, lane + v * g.lanes, param_is_bf16(g, which));
+            return norm_param<ANY>(g, which, at.col(v));
         }
     };
 
@@ -300,13 +310,16 @@ hipError_t launch_fwd(const ResidualNormParams& p, hipStream_t st)
         const int64_t span = (teams + 1) * (gate_rows ? g.team_rows : 1);                // rows that a workgroup's teams reach over
         any = p.cols % 8 != 0 || !by_descriptor(p.x, p.x_bf16, p.ldx, span) || !by_descriptor(p.u, p.u_bf16, p.ldu, span) ||
               !by_descriptor(p.h, p.x_bf16, p.ldh, span) || !by_descriptor(p.y, p.u_bf16, p.ldy, span);
-        lds = s.v == 1 || s.v == 4 ? 0 : param_bytes(s, any, p.post, p.gate != nullptr, true, false, gate_rows ? teams : 0);
+        lds = s.v == 1 ? 0 :
+              s.v == 4 ? give_planes(g, s, {{P_PRE_WEIGHT, p.y || p.y_codes}, {P_POST_WEIGHT, p.post}, {P_GATE, p.gate && !gate_rows},
+                                            {P_PRE_BIAS, p.layer && (p.y || p.y_codes)}, {P_POST_BIAS, p.layer && p.post}}) :
+                         param_bytes(s, any, p.post, p.gate != nullptr, p.layer, false, gate_rows ? teams : 0);
         if (lds <= NORM_LDS_MAX) break;
         s = four_vectors(p.cols);
     }
     const uint32_t threads = teams * s.lanes;
     hipError_t e = hipSuccess;
-    by_vectors<true>(s.v, [&](auto v) {
+    by_vectors(s.v, [&](auto v) {
         by_kind(any, p.post, p.gate != nullptr, [&](auto post, auto gate, auto odd) {
             auto run = [&](auto eight) {
                 e = start_norm(residual_norm_fwd_kernel<XT, UT, decltype(v)::value, decltype(post)::value, decltype(gate)::value,
@@ -322,19 +335,21 @@ hipError_t launch_fwd(const ResidualNormParams& p, hipStream_t st)
 // Shape of a backward launch, the same for every type.
 struct BwdPlan {
     TeamShape shape;
-    uint32_t teams_per_block, grid;
+    uint32_t teams_per_block, grid, strips;
     int64_t teams, pieces, team_rows;        // pieces 0: teams own whole gate rows
+    bool halves;                             // rows first, then sums (strips of columns, a wave each)
 };
 
 BwdPlan plan_bwd(int64_t rows, int64_t cols, int64_t gate_rows)
 {
     BwdPlan b{};
     b.shape = shape_for(cols, 2);
-    const uint32_t lanes = b.shape.lanes, most = NORM_THREADS / lanes, grid = UNITS;      // 8 waves on a unit: few sums to add up
+    b.halves = b.shape.v == 4;
+    if (b.halves) b.shape = {64, 1};
+    b.strips = b.halves ? (uint32_t)((cols + 511) / 512) : 1;
+    const uint32_t lanes = b.shape.lanes, most = NORM_THREADS / lanes, grid = UNITS / b.strips;      // 8 waves on a unit: few sums to add up
     b.teams_per_block = (uint32_t)std::min<int64_t>(most, std::max<int64_t>(1, (rows + grid - 1) / grid));
     b.teams_per_block = whole_waves(b.teams_per_block, lanes);
-    // the largest that any kind of kernel takes; then one team is a workgroup
-    if (param_bytes(b.shape, true, true, true, true, true, b.teams_per_block) > NORM_LDS_MAX) { b.shape = four_vectors(cols); b.teams_per_block = 1; }
     const int64_t teams = std::min<int64_t>(rows, (int64_t)grid * b.teams_per_block), run = rows / gate_rows;
     if (gate_rows == 1 || 2 * gate_rows <= teams) {
         b.pieces = std::min(run, teams / gate_rows);
@@ -361,7 +376,7 @@ size_t residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_ro
 {
     const BwdPlan b = plan_bwd(rows, cols, std::max<int64_t>(1, gate_rows));
     const int64_t gate = gate_rows > 1 ? (b.pieces > 0 ? b.teams : 0) : b.grid;
-    return ((size_t)SUMS * b.grid + (size_t)gate) * (size_t)cols * sizeof(float);
+    return (b.halves ? (size_t)rows * sizeof(float2) : 0) + ((size_t)SUMS * b.grid + (size_t)gate) * (size_t)cols * sizeof(float);
 }
 
 hipError_t launch_residual_norm_bwd(const ResidualNormParams& p, const ResidualNormGrads& d, hipStream_t st)
@@ -373,21 +388,17 @@ hipError_t launch_residual_norm_bwd(const ResidualNormParams& p, const ResidualN
     const bool any = p.cols % 8 != 0 || !by_descriptor(d.dh, p.x_bf16, d.lddh, span) || !by_descriptor(d.dy, p.u_bf16, d.lddy, span) ||
                      !by_descriptor(d.dx, p.x_bf16, d.lddx, span) || !by_descriptor(d.du, p.u_bf16, d.lddu, span) ||
                      (!eight && (!by_descriptor(p.h, p.x_bf16, p.ldh, span) || !by_descriptor(p.u, p.u_bf16, p.ldu, span)));
+    const auto launch = p.layer ? launch_norm_bwd_layer : launch_norm_bwd_rms;
     NormGradArgs a{};
     a.f = norm_args(p, b.shape);
     a.dh = d.dh; a.dy = d.dy; a.dx = d.dx; a.du = d.du;
     a.lddh = d.lddh; a.lddy = d.lddy; a.lddx = d.lddx; a.lddu = d.lddu;
-    a.partials = static_cast<float*>(d.workspace);
+    a.means = static_cast<float2*>(d.workspace);
+    a.partials = static_cast<float*>(d.workspace) + (b.halves ? 2 * p.rows : 0);
     a.gate_partials = a.partials + (int64_t)SUMS * b.grid * p.cols;
     a.dgate = d.dgate;
     a.gate_rows = gate_rows; a.pieces = b.pieces;
-    a.f.teams = b.teams; a.f.team_rows = b.team_rows; a.f.row_step = gate_rows > 1 ? 1 : b.teams;
     a.want_gate = p.gate != nullptr && d.dgate != nullptr;
-    const uint32_t threads = b.teams_per_block * b.shape.lanes, width = b.shape.lanes * b.shape.v * 8;
-    size_t lds = b.shape.v == 4 ? 0 : param_bytes(b.shape, any, p.post, p.gate != nullptr, p.layer, true, a.f.gate_by_row ? b.teams_per_block : 0);
-    if (b.teams_per_block > 1) lds = std::max(lds, (size_t)b.teams_per_block * width * sizeof(float));
-    hipError_t e = (p.layer ? launch_norm_bwd_layer : launch_norm_bwd_rms)(a, p.x_bf16, p.u_bf16, eight, any, b.shape.v, b.grid, threads, lds, st);
-    if (e != hipSuccess) return e;
     NormFinishArgs f{};
     f.partials = a.partials; f.gate_partials = a.gate_partials;
     f.parts = b.grid; f.gate_parts = gate_rows > 1 ? (uint32_t)b.pieces : b.grid; f.cols = (uint32_t)p.cols;
@@ -398,7 +409,28 @@ hipError_t launch_residual_norm_bwd(const ResidualNormParams& p, const ResidualN
     const uint32_t gates = f.out[GATE_SUM] ? (uint32_t)gate_rows : 0;
     bool wanted = gates > 0;
     for (void* o : f.out) wanted = wanted || o != nullptr;
-    if (!wanted) return hipSuccess;
+
+    hipError_t e = hipSuccess;
+    if (b.halves) {
+        const TeamShape s = four_vectors(p.cols);
+        NormGradArgs r = a;
+        r.f = norm_args(p, s);
+        const uint32_t grid = (uint32_t)std::min<int64_t>(p.rows, UNITS);
+        r.f.teams = r.f.row_step = grid;
+        r.f.team_rows = (p.rows + grid - 1) / grid;
+        const size_t lds = give_planes(r.f, s, {{P_PRE_WEIGHT, d.dy != nullptr}, {P_POST_WEIGHT, p.post}, {P_GATE, p.gate && gate_rows == 1}});
+        e = launch(r, p.x_bf16, p.u_bf16, eight, any, s.v, BWD_ROWS, grid, s.lanes, lds, st);
+        if (e != hipSuccess || (!wanted && !a.want_gate)) return e;
+    }
+    a.f.teams = b.teams; a.f.team_rows = b.team_rows; a.f.row_step = gate_rows > 1 ? 1 : b.teams;
+    const uint32_t threads = b.teams_per_block * b.shape.lanes, width = b.shape.lanes * b.shape.v * 8;
+    // the parameters, with the teams' gate rows where there is room for them; at the end the sums
+    auto bytes = [&](uint32_t own) { return param_bytes(b.shape, any, p.post, p.gate != nullptr, p.layer, true, own); };
+    a.f.gate_in_lds = a.f.gate_by_row && bytes(b.teams_per_block) <= NORM_LDS_MAX;
+    size_t lds = bytes(a.f.gate_in_lds ? b.teams_per_block : 0);
+    if (b.teams_per_block > 1) lds = std::max(lds, (size_t)b.teams_per_block * width * sizeof(float));
+    e = launch(a, p.x_bf16, p.u_bf16, eight, any, b.shape.v, b.halves ? BWD_SUMS : BWD_ALL, dim3(b.grid, b.strips), threads, lds, st);
+    if (e != hipSuccess || !wanted) return e;
     residual_norm_finish_kernel<<<(uint32_t)((p.cols + 31) / 32) * (SUMS - 1 + gates), 32 * FINISH_RUNS, 0, st>>>(f);
     return hipGetLastError();
 }

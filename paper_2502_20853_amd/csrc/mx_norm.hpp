@@ -15,6 +15,8 @@
 #include "mx_block.hpp"
 
 #include <algorithm>
+#include <initializer_list>
+#include <utility>
 
 namespace mxl {
 
@@ -41,7 +43,9 @@ struct NormArgs {
     int64_t teams, team_rows, row_step;                       // teams of the launch, the most rows that one has, from one to the next
     uint32_t cols, pitch8, lanes;
     float inv_cols, rho, sigma, eps;
+    uint8_t plane[8];                                         // of the parameters in LDS (ParamPlanes)
     bool layer, post, param_bf16, gate_bf16, gate_by_row, floor_mode;
+    bool gate_in_lds;                                         // the teams' gate rows
 };
 
 struct NormGradArgs {
@@ -53,10 +57,15 @@ struct NormGradArgs {
     int64_t lddh, lddy, lddx, lddu;
     float* partials;          // [SUMS][workgroups][cols]
     float* gate_partials;     // [gate rows x pieces][cols], or [workgroups][cols] for a gate of one row
+    float2* means;            // of each row, between the two halves
     void* dgate;              // where whole gate rows belong to one team
     int64_t gate_rows, pieces;                                // pieces 0: teams own whole gate rows
     bool want_gate;
 };
+
+// What a backward kernel does: the whole pass, or for rows so wide that the sums and a row do not fit in registers its two halves: the
+// gradients of the rows, and then (from the means of the rows that these leave) the sums, a strip of columns at a time.
+enum BwdPart { BWD_ALL, BWD_ROWS, BWD_SUMS };
 
 enum NormSum { PRE_WEIGHT, POST_WEIGHT, GATE_SUM, PRE_BIAS, POST_BIAS, SUMS };
 enum NormParam { P_PRE_WEIGHT, P_POST_WEIGHT, P_GATE, P_PRE_BIAS, P_POST_BIAS, PARAMS };
@@ -79,8 +88,11 @@ struct ParamLds {
     {
         return p == P_PRE_WEIGHT ? 0 : p == P_POST_WEIGHT ? 1 : p == P_GATE ? GATE_SLOT : p == P_PRE_BIAS ? PRE_BIAS_SLOT : POST_BIAS_SLOT;
     }
-    static __device__ __forceinline__ void put(float* lds, NormParam p, uint32_t vector, const F8& f) { put(lds + vector * STRIDE + slot(p) * 8, f); }
-    static __device__ __forceinline__ F8 get(const float* lds, NormParam p, uint32_t vector) { return get(lds + vector * STRIDE + slot(p) * 8); }
+    static __device__ __forceinline__ void put(float* lds, uint32_t stride, NormParam p, uint32_t vector, const F8& f)
+    {
+        put(lds + vector * stride + slot(p) * 8, f);
+    }
+    static __device__ __forceinline__ F8 get(const float* lds, uint32_t stride, NormParam p, uint32_t vector) { return get(lds + vector * stride + slot(p) * 8); }
     static __device__ __forceinline__ void put(float* at, const F8& f)
     {
         float4* to = reinterpret_cast<float4*>(at);
@@ -94,6 +106,35 @@ struct ParamLds {
         return F8{{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}};
     }
 };
+
+// The same for rows so wide that they do not fit in that form: a plane of 16 bytes for each eight columns where a parameter is
+// bfloat16, two where it is FP32, for as many as there is room for.  The rest are read from cache (NO_PLANE).
+struct ParamPlanes {
+    static constexpr uint8_t NO_PLANE = 0xFF;
+    static __device__ __forceinline__ void put(float* lds, uint32_t plane, uint32_t vectors, uint32_t vector, bool bf16, const F8& f)
+    {
+        uint4* to = reinterpret_cast<uint4*>(lds) + plane * vectors + vector;
+        if (bf16) {
+            RawBf16 r;
+            narrow(f, r);                                                // exact: it came from there
+            to[0] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+        } else {
+            to[0] = make_uint4(__float_as_uint(f.v[0]), __float_as_uint(f.v[1]), __float_as_uint(f.v[2]), __float_as_uint(f.v[3]));
+            to[vectors] = make_uint4(__float_as_uint(f.v[4]), __float_as_uint(f.v[5]), __float_as_uint(f.v[6]), __float_as_uint(f.v[7]));
+        }
+    }
+    static __device__ __forceinline__ F8 get(const float* lds, uint32_t plane, uint32_t vectors, uint32_t vector, bool bf16)
+    {
+        const uint4* from = reinterpret_cast<const uint4*>(lds) + plane * vectors + vector;
+        const uint4 a = from[0];
+        if (bf16) return widen(RawBf16{{a.x, a.y, a.z, a.w}});
+        const uint4 b = from[vectors];
+        return F8{{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                   __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)}};
+    }
+};
+
+__device__ __forceinline__ bool param_is_bf16(const NormArgs& g, NormParam which) { return which == P_GATE ? g.gate_bf16 : g.param_bf16; }
 
 // A parameter's eight values from `col` on, from memory.
 template <bool TAIL>
@@ -126,7 +167,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const void* base, i
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + bytes, (short)0, base == nullptr ? 0 : (int)OFF_MAX, 0x00020000);
 }
 
-constexpr int NT = 2;                                    // the nontemporal bit: what is loaded is not read again soon
+constexpr int NT = 2;                                    // the nontemporal bit: loads that are not repeated soon, and 8-bit checkpoints
 
 __device__ __forceinline__ RawBf16 buffer_load_raw(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t step, uint16_t)
 {
@@ -196,7 +237,7 @@ __device__ __forceinline__ void store_codes8(uint8_t* codes, uint8_t* scales, co
     const Codes8 c = pack8(f, byte);
     const bool in = at.in<V>(v, at.pitch8);
     const uint32_t groups = at.pitch8 >> 5;
-    __builtin_amdgcn_raw_buffer_store_b64(u2_vec{c.w[0], c.w[1]}, descriptor(codes, at.first * at.pitch8), in ? at.behind * at.pitch8 + at.col0 : OFF_END, v * at.step, 0);
+    __builtin_amdgcn_raw_buffer_store_b64(u2_vec{c.w[0], c.w[1]}, descriptor(codes, at.first * at.pitch8), in ? at.behind * at.pitch8 + at.col0 : OFF_END, v * at.step, NT);
     __builtin_amdgcn_raw_buffer_store_b8((uint8_t)byte, descriptor(scales, at.first * groups),
                                          in && (at.col0 & 31u) == 0 ? at.behind * groups + (at.col0 >> 5) : OFF_END, v * at.step >> 5, 0);
 }
@@ -285,13 +326,13 @@ void by_kind(bool any, bool post, bool gate, F&& f)
     else if (post) gate ? f(Y{}, Y{}, N{}) : f(Y{}, N{}, N{});
     else           gate ? f(N{}, Y{}, N{}) : f(N{}, N{}, N{});
 }
-template <bool THREE, typename F>
+template <typename F>
 void by_vectors(int v, F&& f)
 {
     if (v == 1)      f(std::integral_constant<int, 1>{});
     else if (v == 2) f(std::integral_constant<int, 2>{});
-    else if (v == 4) f(std::integral_constant<int, 4>{});
-    else if constexpr (THREE) f(std::integral_constant<int, 3>{});
+    else if (v == 3) f(std::integral_constant<int, 3>{});
+    else             f(std::integral_constant<int, 4>{});
 }
 
 // Whether a matrix's rows go through descriptors: `rows` of them from a workgroup's first one on.
@@ -313,9 +354,24 @@ inline size_t param_bytes(const TeamShape& s, bool any, bool post, bool gate, bo
     return (words + (size_t)own_gates * 12) * s.lanes * s.v * sizeof(float);
 }
 
+// Gives planes to the parameters that a kernel reads, in the order of `wanted`, and returns their bytes.
+inline size_t give_planes(NormArgs& g, const TeamShape& s, std::initializer_list<std::pair<NormParam, bool>> wanted)
+{
+    const size_t bytes = (size_t)s.lanes * s.v * 16;
+    size_t planes = 0;
+    for (uint8_t& p : g.plane) p = ParamPlanes::NO_PLANE;
+    for (const auto& [which, there] : wanted) {
+        const size_t n = (which == P_GATE ? g.gate_bf16 : g.param_bf16) ? 1 : 2;
+        if (!there || (planes + n) * bytes > NORM_LDS_MAX) continue;
+        g.plane[which] = (uint8_t)planes;
+        planes += n;
+    }
+    return planes * bytes;
+}
+
 // Starts a kernel with `lds` bytes, asking for more than a kernel may have by itself where need be.
 template <typename K, typename A>
-hipError_t start_norm(K kernel, uint32_t grid, uint32_t threads, size_t lds, hipStream_t st, const A& args)
+hipError_t start_norm(K kernel, dim3 grid, uint32_t threads, size_t lds, hipStream_t st, const A& args)
 {
     if (lds > 65536 - sizeof(TeamScratch)) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -326,7 +382,7 @@ hipError_t start_norm(K kernel, uint32_t grid, uint32_t threads, size_t lds, hip
 }
 
 // The backward kernels by norm (a file each).
-hipError_t launch_norm_bwd_rms(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, uint32_t grid, uint32_t threads, size_t lds, hipStream_t st);
-hipError_t launch_norm_bwd_layer(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, uint32_t grid, uint32_t threads, size_t lds, hipStream_t st);
+hipError_t launch_norm_bwd_rms(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, BwdPart part, dim3 grid, uint32_t threads, size_t lds, hipStream_t st);
+hipError_t launch_norm_bwd_layer(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, BwdPart part, dim3 grid, uint32_t threads, size_t lds, hipStream_t st);
 
 }  // namespace mxl

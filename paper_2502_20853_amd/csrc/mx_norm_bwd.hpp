@@ -24,14 +24,21 @@ template <typename T> __device__ __forceinline__ void renew(Kept<T, false>& k) {
 enum RowMode { ROW_AGAIN, ROW_HELD, ROW_AHEAD };
 
 // By the registers that the sums, the raw row (twice) and the gradient that is passed on take, of the 256 a lane has.
-template <typename XT, typename UT, int V, bool POST, bool GATE, bool LAYER, bool CKPT>
-constexpr RowMode row_mode()
+// keep: also whether that gradient is kept between the second step and the third, or computed again.
+struct RowPlan {
+    RowMode mode;
+    bool keep;
+};
+template <typename XT, typename UT, int V, bool POST, bool GATE, bool LAYER, bool CKPT, BwdPart PART>
+constexpr RowPlan row_plan()
 {
     constexpr int x = sizeof(XT) * 2, u = sizeof(UT) * 2;               // registers of eight values
-    constexpr int sums = (LAYER ? 2 : 1) * (POST ? 2 : 1) + GATE;
+    constexpr int sums = PART == BWD_ROWS ? 0 : (LAYER ? 2 : 1) * (POST ? 2 : 1) + GATE;
     constexpr int raw = u + x + (CKPT ? 3 : x) + (!POST && !GATE ? 0 : CKPT ? 3 : u);
-    constexpr int fixed = V * (8 * sums + (POST ? 8 : 0)) + 76;
-    return fixed + 2 * V * raw <= 240 ? ROW_AHEAD : fixed + V * raw <= 240 ? ROW_HELD : ROW_AGAIN;
+    constexpr int fixed = V * 8 * sums + 76, kept = POST ? V * 8 : 0;
+    if (fixed + kept + 2 * V * raw <= 240) return {ROW_AHEAD, true};
+    if (fixed + kept + V * raw <= 240) return {ROW_HELD, true};
+    return {fixed + V * raw <= 240 ? ROW_HELD : ROW_AGAIN, false};
 }
 
 // Backward pass.  A team owns a run of rows and adds its part of the parameters' gradients in registers, row by row; the
@@ -41,7 +48,7 @@ constexpr RowMode row_mode()
 // Up to nine FP32 vectors of the row's length would live in registers: the sums do, the parameters are read from LDS
 // (with four vectors a lane from cache), and what a row needs again behind its sums is kept as loaded.  What is missing (a
 // gradient, a weight) reads as zero or one, so that the loop has next to no branches.
-template <typename XT, typename UT, int V, bool POST, bool GATE, bool LAYER, bool CKPT, bool ANY>
+template <typename XT, typename UT, int V, bool POST, bool GATE, bool LAYER, bool CKPT, bool ANY, BwdPart PART>
 __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const NormGradArgs a)
 {
     extern __shared__ float lds[];               // the parameters; at the end [teams][width] for the sums
@@ -50,13 +57,14 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
     const uint32_t team_in_block = threadIdx.x / g.lanes, lane = threadIdx.x % g.lanes;
     const uint32_t teams = blockDim.x / g.lanes;
     Team team{g.lanes, team_in_block * (g.lanes >> 6), &scratch};
-    const uint32_t step = g.lanes * 8u, col0 = lane * 8u, width = step * V, vectors = g.lanes * V;
+    const uint32_t step = g.lanes * 8u, width = step * V, vectors = g.lanes * V;
+    const uint32_t base = PART == BWD_SUMS ? blockIdx.y * width : 0u, col0 = base + lane * 8u;           // of the strip
     constexpr bool READ_U = POST || GATE;
     const bool post = POST && (!ANY || g.post), gate_by_row = GATE && g.gate_by_row;
 
     const int64_t k0 = (int64_t)blockIdx.x * teams, k = k0 + team_in_block;
     // without gate rows every g.teams-th row, as in the forward pass
-    const bool whole = GATE && a.pieces == 0, runs = GATE && g.row_step == 1;
+    const bool whole = GATE && a.pieces == 0, runs = PART != BWD_ROWS && GATE && g.row_step == 1;
     auto start_of = [&](int64_t k) {                                     // of a run
         if (whole) return a.gate_rows * k / g.teams * g.gate_run;
         const int64_t group = k / a.pieces, piece = k % a.pieces;
@@ -66,14 +74,24 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
     const uint32_t count = k >= g.teams ? 0u : (uint32_t)(runs ? start_of(k + 1) - begin : (g.rows - k + g.teams - 1) / g.teams);
 
     using Params = ParamLds<POST, GATE, LAYER, true>;
-    if constexpr (V < 4) {
+    if constexpr (PART != BWD_ROWS) {
         auto fill = [&](NormParam which) {
-            for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x) Params::put(lds, which, c, norm_param<ANY>(g, which, c * 8));
+            for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x) Params::put(lds, Params::STRIDE, which, c, norm_param<ANY>(g, which, base + c * 8));
         };
         fill(P_PRE_WEIGHT);
         if (POST) fill(P_POST_WEIGHT);
         if (GATE && !gate_by_row) fill(P_GATE);
         if (POST && LAYER) fill(P_POST_BIAS);
+        __syncthreads();
+    } else {
+        auto fill = [&](NormParam which) {
+            if (g.plane[which] == ParamPlanes::NO_PLANE) return;
+            for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x)
+                ParamPlanes::put(lds, g.plane[which], vectors, c, param_is_bf16(g, which), norm_param<ANY>(g, which, c * 8));
+        };
+        fill(P_PRE_WEIGHT);
+        if (POST) fill(P_POST_WEIGHT);
+        if (GATE) fill(P_GATE);
         __syncthreads();
     }
 
@@ -83,7 +101,8 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[s][v] = mxd::zero8();
 
-    constexpr RowMode MODE = row_mode<XT, UT, V, POST, GATE, LAYER, CKPT>();
+    constexpr RowPlan PLAN = row_plan<XT, UT, V, POST, GATE, LAYER, CKPT, PART>();
+    constexpr RowMode MODE = PLAN.mode;
     struct Vec {                                                         // a lane's part of a row, as loaded
         Raw<UT> dy;
         Raw<XT> dh;
@@ -102,6 +121,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
     };
     Vec next[MODE == ROW_AHEAD ? V : 1];
     float4 sn;
+    float2 mn = make_float2(0.0f, 0.0f);
     auto fetch = [&](const Place& at) {
         if constexpr (MODE == ROW_AHEAD) {
 #pragma unroll
@@ -110,6 +130,11 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
         const u4_vec s = __builtin_amdgcn_raw_buffer_load_b128(descriptor(g.stats, at.first * (int64_t)sizeof(float4)),
                                                                at.live ? at.behind * (uint32_t)sizeof(float4) : OFF_END, 0, 0);
         sn = make_float4(__uint_as_float(s.x), __uint_as_float(s.y), __uint_as_float(s.z), __uint_as_float(s.w));
+        if constexpr (PART == BWD_SUMS) {
+            const u2_vec m = __builtin_amdgcn_raw_buffer_load_b64(descriptor(a.means, at.first * (int64_t)sizeof(float2)),
+                                                                  at.live ? at.behind * (uint32_t)sizeof(float2) : OFF_END, 0, 0);
+            mn = make_float2(__uint_as_float(m.x), __uint_as_float(m.y));
+        }
     };
     int64_t gate_row = 0, in_run = 0;
     if (gate_by_row && count > 0) {
@@ -121,23 +146,28 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
     float* own_gate = lds + vectors * Params::STRIDE + team_in_block * vectors * Params::GATE_STRIDE;     // a lane reads what it wrote
     auto gate_of_row = [&](int v) { return param8<ANY>(g.gate, g.gate_bf16, gate_row * g.ld_gate + at.col(v), at.left(v), 0.0f); };
     auto take_gate = [&]() {
-        if constexpr (V < 4) {
+        if (PART != BWD_ROWS && g.gate_in_lds) {
 #pragma unroll
             for (int v = 0; v < V; ++v) Params::put(own_gate + (lane + v * g.lanes) * Params::GATE_STRIDE, gate_of_row(v));
         }
     };
     if (gate_by_row) take_gate();
     auto param = [&](NormParam which, int v) {
-        if constexpr (V < 4) {
-            if (which == P_GATE && gate_by_row) return Params::get(own_gate + (lane + v * g.lanes) * Params::GATE_STRIDE);
-            return Params::get(lds, which, lane + v * g.lanes);
+        if constexpr (PART != BWD_ROWS) {
+            if (which == P_GATE && gate_by_row)
+                return g.gate_in_lds ? Params::get(own_gate + (lane + v * g.lanes) * Params::GATE_STRIDE) : gate_of_row(v);
+            return Params::get(lds, Params::STRIDE, which, lane + v * g.lanes);
         } else {
-            return which == P_GATE && gate_by_row ? gate_of_row(v) : norm_param<ANY>(g, which, col0 + v * step);
+            if (which == P_GATE && gate_by_row) return gate_of_row(v);
+            if (g.plane[which] != ParamPlanes::NO_PLANE) return ParamPlanes::get(lds, g.plane[which], vectors, lane + v * g.lanes, param_is_bf16(g, which));
+            return norm_param<ANY>(g, which, col0 + v * step);
         }
     };
     for (uint32_t i = 0; i < (uint32_t)g.team_rows; ++i) {
         Vec held[MODE == ROW_AGAIN ? 1 : V];
         const float4 st = sn;
+        const float2 means = mn;
+        if (PART == BWD_ROWS && gate_by_row && at.live) gate_row = at.row() / g.gate_run;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if constexpr (MODE == ROW_AHEAD) held[v] = next[v];
@@ -164,14 +194,21 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
                 const float n = (h.v[t] - st.z) * st.w, b = dy.v[t] * w.v[t];
-                acc[PRE_WEIGHT][v].v[t] = __builtin_fmaf(dy.v[t], n, acc[PRE_WEIGHT][v].v[t]);
-                if (LAYER) acc[PRE_BIAS][v].v[t] += dy.v[t];
+                if constexpr (PART != BWD_ROWS) {
+                    acc[PRE_WEIGHT][v].v[t] = __builtin_fmaf(dy.v[t], n, acc[PRE_WEIGHT][v].v[t]);
+                    if (LAYER) acc[PRE_BIAS][v].v[t] += dy.v[t];
+                }
                 s[0] = __builtin_fmaf(b, n, s[0]);
                 if (LAYER) s[1] += b;
             }
         });
-        team.sum<LAYER ? 2 : 1>(s);
-        const float h1 = s[0] * g.inv_cols, h0 = s[1] * g.inv_cols;
+        float h1 = means.x, h0 = means.y;
+        if constexpr (PART != BWD_SUMS) {
+            team.sum<LAYER ? 2 : 1>(s);
+            h1 = s[0] * g.inv_cols;
+            h0 = s[1] * g.inv_cols;
+        }
+        if (PART == BWD_ROWS && lane == 0 && at.live) a.means[at.row()] = make_float2(h1, h0);
         forget();
         s[0] = s[1] = 0.0f;
         // the gradient of h from the vector's parts
@@ -187,14 +224,16 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
             }
             return dh;
         };
-        F8 dv[MODE == ROW_AGAIN || !POST ? 1 : V];
+        F8 dv[PLAN.keep && POST ? V : 1];
         const float ru = post ? st.y : 1.0f;                             // without a post-norm u itself takes part
-        each(true, true, [&](Vec& r, int v) {
+        if constexpr (PART != BWD_SUMS || READ_U) each(true, true, [&](Vec& r, int v) {
             const F8 dh = gradient(r, v);
-            F8 out;
+            if constexpr (PART != BWD_SUMS) {
+                F8 out;
 #pragma unroll
-            for (int t = 0; t < 8; ++t) out.v[t] = g.rho * dh.v[t];
-            store_vec<ANY, V, XT>(a.dx, a.lddx, at, v, out);
+                for (int t = 0; t < 8; ++t) out.v[t] = g.rho * dh.v[t];
+                store_vec<ANY, V, XT>(a.dx, a.lddx, at, v, out);
+            }
             F8 d, u, w;
 #pragma unroll
             for (int t = 0; t < 8; ++t) d.v[t] = g.sigma * dh.v[t];
@@ -218,25 +257,27 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
                 }
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
-                    acc[GATE_SUM][v].v[t] = __builtin_fmaf(d.v[t], value.v[t], acc[GATE_SUM][v].v[t]);
+                    if constexpr (PART != BWD_ROWS) acc[GATE_SUM][v].v[t] = __builtin_fmaf(d.v[t], value.v[t], acc[GATE_SUM][v].v[t]);
                     d.v[t] *= gate.v[t];
                 }
             }
             if constexpr (!POST) {
-                store_vec<ANY, V, UT>(a.du, a.lddu, at, v, d);
+                if constexpr (PART != BWD_SUMS) store_vec<ANY, V, UT>(a.du, a.lddu, at, v, d);
             } else {
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
-                    acc[POST_WEIGHT][v].v[t] = __builtin_fmaf(d.v[t], u.v[t], acc[POST_WEIGHT][v].v[t]);
-                    if (LAYER) acc[POST_BIAS][v].v[t] += d.v[t];
+                    if constexpr (PART != BWD_ROWS) {
+                        acc[POST_WEIGHT][v].v[t] = __builtin_fmaf(d.v[t], u.v[t], acc[POST_WEIGHT][v].v[t]);
+                        if (LAYER) acc[POST_BIAS][v].v[t] += d.v[t];
+                    }
                     d.v[t] *= w.v[t];
                     s[0] = __builtin_fmaf(d.v[t], u.v[t], s[0]);
                     if (LAYER) s[1] += d.v[t];
                 }
-                if constexpr (MODE != ROW_AGAIN) dv[v] = d;
+                if constexpr (PLAN.keep) dv[v] = d;
             }
         });
-        if constexpr (POST) {
+        if constexpr (POST && PART != BWD_SUMS) {
             float u1 = 0.0f, u0 = 0.0f;
             if (post) {
                 team.sum<LAYER ? 2 : 1>(s);
@@ -246,7 +287,8 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
             forget();
             each(true, true, [&](Vec& r, int v) {
                 F8 d;
-                if constexpr (MODE == ROW_AGAIN) {
+                if constexpr (!PLAN.keep) {
+                    renew(r.dh);
                     d = gradient(r, v);
                     const F8 w = param(P_POST_WEIGHT, v);
 #pragma unroll
@@ -268,7 +310,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
                 store_vec<ANY, V, UT>(a.du, a.lddu, at, v, d);
             });
         }
-        if (gate_by_row && ++in_run == g.gate_run) {       // the gate's row is complete
+        if (PART != BWD_ROWS && gate_by_row && ++in_run == g.gate_run) {       // the gate's row is complete
             if (whole && a.want_gate) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
@@ -285,6 +327,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
         }
         at = ahead;
     }
+    if constexpr (PART == BWD_ROWS) return;
 
 #pragma unroll
     for (int s = 0; s < SUMS; ++s) {
@@ -311,27 +354,32 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
         }
         __syncthreads();
 #pragma unroll
-        for (int v = 0; v < V; ++v) store_raw<false>(lds + team_in_block * width + col0 + v * step, acc[s][v], 8);
+        for (int v = 0; v < V; ++v) store_raw<false>(lds + team_in_block * width + (lane + v * g.lanes) * 8u, acc[s][v], 8);
         __syncthreads();
-        for (uint32_t c = threadIdx.x; c < g.cols; c += blockDim.x) {
+        for (uint32_t c = threadIdx.x; c < width && base + c < g.cols; c += blockDim.x) {
             float t = lds[c];
             for (uint32_t i = 1; i < teams; ++i) t += lds[i * width + c];
-            out[c] = t;
+            out[base + c] = t;
         }
     }
 }
 
 template <bool LAYER>
-hipError_t launch_norm_bwd(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, uint32_t grid, uint32_t threads, size_t lds, hipStream_t st)
+hipError_t launch_norm_bwd(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, BwdPart part, dim3 grid, uint32_t threads, size_t lds, hipStream_t st)
 {
     hipError_t e = hipSuccess;
     by_types(x_bf16, u_bf16, [&](auto xt, auto ut) {
-        by_vectors<false>(v, [&](auto n) {
-            by_kind(any, a.f.post, a.f.gate != nullptr, [&](auto post, auto gate, auto odd) {
-                by_flag(eight, [&](auto c) {
+        by_kind(any, a.f.post, a.f.gate != nullptr, [&](auto post, auto gate, auto odd) {
+            by_flag(eight, [&](auto c) {
+                auto run = [&](auto n, auto which) {
                     e = start_norm(residual_norm_bwd_kernel<decltype(xt), decltype(ut), decltype(n)::value, decltype(post)::value, decltype(gate)::value,
-                                                            LAYER, decltype(c)::value, decltype(odd)::value>, grid, threads, lds, st, a);
-                });
+                                                            LAYER, decltype(c)::value, decltype(odd)::value, decltype(which)::value>, grid, threads, lds, st, a);
+                };
+                using One = std::integral_constant<int, 1>;
+                if (part == BWD_ROWS)      run(std::integral_constant<int, 4>{}, std::integral_constant<BwdPart, BWD_ROWS>{});
+                else if (part == BWD_SUMS) run(One{}, std::integral_constant<BwdPart, BWD_SUMS>{});
+                else if (v == 1)           run(One{}, std::integral_constant<BwdPart, BWD_ALL>{});
+                else                       run(std::integral_constant<int, 2>{}, std::integral_constant<BwdPart, BWD_ALL>{});
             });
         });
     });

@@ -162,6 +162,27 @@ def test_residual_norm_many_rows(mx, n, d):
         run_case(mx, n, d, BF, BF, F32, layer, True, 1, ckpt, 3)
 
 
+@pytest.mark.parametrize("n,d,gates", [(600, 8192, 2), (600, 8192, 600), (300, 8200, 300), (300, 8200, 3), (300, 9001, 5), (130, 16384, 130)])
+def test_wide_rows_with_gate_rows(mx, n, d, gates):
+    for i, (layer, post, ckpt) in enumerate([(False, True, True), (True, True, False), (False, False, False)]):
+        print("wide gates", n, d, gates, i, flush=True)
+        run_case(mx, n, d, F32 if i == 1 else BF, BF, BF, layer, post, gates, ckpt, 90 + i)
+
+
+@pytest.mark.parametrize("d", [8200, 10000])
+def test_wide_rows_whose_inputs_alone_want_gradients(mx, d):
+    g = torch.Generator(device="cuda").manual_seed(95)
+    x, u, p = make(g, 70, d, BF, BF, BF, False, True, 5)
+    gr = torch.randn((2, 70, d), generator=g, device="cuda").to(BF)
+    every = [t.requires_grad_(True) for t in (x, u, *p.values())]
+    want = torch.autograd.grad(mx.residual_norm(x, u, **p, post=True), every, (gr[0], gr[1]))
+    plain = {k: v.detach() for k, v in p.items()}
+    got = torch.autograd.grad(mx.residual_norm(x, u, **plain, post=True), (x, u), (gr[0], gr[1]))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    (gate,) = torch.autograd.grad(mx.residual_norm(x, u, **{**plain, "gate": p["gate"]}, post=True), (p["gate"],), (gr[0], gr[1]))
+    assert torch.equal(gate, want[-1])
+
+
 @pytest.mark.parametrize("use", [("h",), ("y",)])
 @pytest.mark.parametrize("ckpt", [False, True])
 def test_one_gradient_is_missing(mx, use, ckpt):
@@ -460,6 +481,20 @@ def test_activation_strides_and_shapes(mx):
         want_g = torch.autograd.grad(mx.activation(r, "silu", gated=True, checkpoint=ckpt), r, torch.ones((15, 72), device="cuda", dtype=BF))[0]
         assert torch.equal(got, want_g)
     assert mx.activation(p[0, 0], "gelu").shape == (144,)
+
+
+@pytest.mark.parametrize("t,n", [(BF, 9001), (F32, 4501)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_activation_gradient_beyond_the_cache(mx, t, n, gated):
+    """A gradient of 295 MB is that of its rows one by one."""
+    g = torch.Generator(device="cuda").manual_seed(12)
+    p = torch.randn((n, 16384), generator=g, device="cuda").to(t)
+    da = torch.randn((n, 16384 // (1 + gated)), generator=g, device="cuda").to(t)
+    for ckpt in (False, True):
+        f = lambda p, da: torch.autograd.grad(mx.activation(p.requires_grad_(True), "silu", gated=gated, checkpoint=ckpt), p, da)[0]
+        whole = f(p, da)
+        for rows in (slice(0, 64), slice(n // 2, n // 2 + 33), slice(n - 65, n)):
+            assert torch.equal(whole[rows], f(p[rows].detach().clone(), da[rows].contiguous()))
 
 
 @pytest.mark.parametrize("gated", [False, True])
