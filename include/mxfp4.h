@@ -393,7 +393,7 @@ int mx_rate_of_change_step(const void* x, int dtype, int64_t rows, int64_t cols,
  *     scales[r][g] = s + 127                          rows x P/32 bytes          past cols hold 0
  *   values   device, dtype F32 or BF16, at the alignment of its elements, ld >= cols
  *   codes    device, 8-byte aligned
- *   1 <= cols, rows * P < 2^35.
+ *   1 <= cols, rows * P <= 2^35 - 2^19.
  * A NaN comes back as NaN; a group that holds an infinity comes back as NaN as a whole; a magnitude of 31/32 * 2^128 or more
  * rounds to 2^128 and comes back as infinity.
  */
@@ -423,7 +423,7 @@ int mx_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, int64_t ro
  *   h8, h8_scales, u8, u8_scales   device out, each pair or NULL: mx_checkpoint_pack of h and of u
  *   stats         device out, FP32 [rows][4], 16-byte aligned, or NULL: mean and r of u, mean and r of h, for the backward
  *                 pass (the mean 0 for MX_NORM_RMS; unspecified where there is no such norm)
- * 1 <= cols <= 16384, rows * cols < 2^35; eps at least 2^-126 (MX_ERR_MODE); pointers at the alignment of their elements
+ * 1 <= cols <= 16384, rows * cols <= 2^35 - 2^19 (cols rounded up to whole groups); eps at least 2^-126 (MX_ERR_MODE); pointers at the alignment of their elements
  * unless stated.  At least one of h and y is asked for.
  */
 enum { MX_NORM_RMS = 0, MX_NORM_LAYER = 1 };
@@ -473,7 +473,8 @@ int mx_residual_norm_fwd(const mx_residual_norm* p, void* stream);
  *   dpre_weight, dpre_bias, dpost_weight, dpost_bias   device out, cols values of param_dtype, each or NULL
  *   dgate       device out, [gate_rows x cols] dense, gate_dtype, or NULL
  *   workspace   device, 16-byte aligned, mx_residual_norm_workspace_bytes(rows, cols, gate_rows) bytes (gate_rows 0
- *               without a gate); MX_ERR_WORKSPACE if NULL or smaller.  Not kept between calls, nothing is cleared.
+ *               without a gate; 0 for sizes that no call takes); MX_ERR_WORKSPACE if NULL or smaller.  Not kept between
+ *               calls, nothing is cleared.
  * Sums over rows run in one fixed order for given sizes, so that a call repeats bit for bit.
  */
 typedef struct mx_residual_norm_grads {
@@ -504,7 +505,7 @@ int mx_residual_norm_bwd(const mx_residual_norm* p, const mx_residual_norm_grads
  *            cols % 32 == 0, a_codes 16-byte aligned)
  *   p8, p8_scales   device out, or NULL: the 8-bit checkpoint of p; gated, that of the matrix [2 rows x cols] whose rows
  *            are the two halves of each row in turn
- *   1 <= cols < 2^30, rows * cols < 2^35 (rounded up to whole groups); pointers at the alignment of their elements, p8 8 bytes.
+ *   1 <= cols < 2^30, rows * cols <= 2^35 - 2^19 (cols rounded up to whole groups); pointers at the alignment of their elements, p8 8 bytes.
  * Backward: dp from da, with p as given or (p8 set) its checkpoint in the place of p:
  *     dp = da act'(p);   gated, with p = [g | w]:   [da w act'(g) | da act(g)].
  */

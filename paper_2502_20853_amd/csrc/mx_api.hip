@@ -566,7 +566,7 @@ static int residual_norm_params(const mx_residual_norm& a, bool branch, mxl::Res
     p.pre_weight = a.pre_weight; p.pre_bias = a.pre_bias; p.post_weight = a.post_weight; p.post_bias = a.post_bias;
     p.param_bf16 = a.param_dtype == MX_DTYPE_BF16;
     p.gate = a.gate; p.gate_bf16 = a.gate_dtype == MX_DTYPE_BF16; p.gate_rows = a.gate_rows; p.ld_gate = a.ld_gate;
-    p.residual_scale = a.residual_scale; p.branch_scale = a.branch_scale; p.eps = a.eps;
+    p.residual_scale = branch ? a.residual_scale : 1.0f; p.branch_scale = branch ? a.branch_scale : 1.0f; p.eps = a.eps;
     p.y_codes = a.y_codes; p.y_scales = a.y_scales; p.floor_mode = a.scale_mode == MX_SCALE_FLOOR;
     p.h8 = a.h8; p.h8_scales = a.h8_scales; p.u8 = a.u8; p.u8_scales = a.u8_scales; p.stats = a.stats;
     return MX_OK;
@@ -591,7 +591,7 @@ int mx_residual_norm_fwd(const mx_residual_norm* a, void* stream)
 
 size_t mx_residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_rows)
 {
-    if (rows <= 0 || cols <= 0 || gate_rows < 0 || gate_rows > rows) return 0;
+    if (rows <= 0 || cols <= 0 || cols > mxl::RESIDUAL_NORM_MAX_COLS || mxl::too_many(rows, cols) || gate_rows < 0 || gate_rows > rows) return 0;
     return mxl::residual_norm_workspace_bytes(rows, cols, gate_rows);
 }
 

@@ -500,17 +500,18 @@ void step_backward(const Tensor& dY, int64_t N, int64_t D, int64_t C, uint64_t s
 
 int dtype_of(const Tensor& t) { return is_bf16(t) ? MX_DTYPE_BF16 : MX_DTYPE_F32; }
 
-// A tensor [..., cols] as rows of unit column stride: itself where it is such a matrix, a dense copy where it is not.
+// A tensor [..., cols] as rows of unit column stride: itself where it is such a matrix, a dense copy where it is not (copy
+// false: a stand-in for checks, with the copy's strides).
 struct Rows {
     Tensor t;
     int64_t rows, cols, ld;
 };
-Rows rows_of(const Tensor& in, int64_t cols)
+Rows rows_of(const Tensor& in, int64_t cols, bool copy = true)
 {
     const int64_t rows = cols > 0 ? in.numel() / cols : 0;
     if (in.dim() == 2 && in.size(1) > 0 && (in.size(1) == 1 || in.stride(1) == 1) && (rows <= 1 || in.stride(0) >= cols))
         return {in, rows, cols, rows <= 1 ? cols : in.stride(0)};
-    return {in.contiguous(), rows, cols, cols};
+    return {copy ? in.contiguous() : in, rows, cols, cols};
 }
 
 void no_trace(const char* what)
@@ -569,6 +570,8 @@ std::pair<Tensor, Tensor> checkpoint_pack(const Tensor& src, const OptTensor& co
     const bool bf16 = is_bf16(src);
     if (src.dim() < 1 || src.numel() == 0) throw Status(fn, MX_ERR_SHAPE);
     at::AutoDispatchBelowADInplaceOrView guard;
+    TORCH_CHECK_VALUE(stream == -1 || rows_of(src, src.size(-1), false).ld != src.size(-1) || src.is_contiguous(),
+                      "on a given stream the values must be rows of unit column stride");          // a copy would be made on the current one
     const Rows r = rows_of(src, src.size(-1));
     mxl::CheckpointParams p{r.t.data_ptr(), bf16, r.rows, r.cols, r.ld, nullptr, nullptr};
     check(mxl::check_checkpoint(p), fn);
@@ -638,23 +641,20 @@ int64_t gate_rows_of(const Tensor& gate, const Tensor& x)
     return rows;
 }
 
-const Tensor dense(const OptTensor& t) { return t ? t->contiguous() : Tensor(); }
-const void* data_of(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
-
 // Everything of a call but its outputs; the tensors it points into live in `keep`.
-mxl::ResidualNormParams norm_params(const NormInputs& in, const NormOptions& o, std::vector<Tensor>& keep)
+mxl::ResidualNormParams norm_params(const NormInputs& in, const NormOptions& o, std::vector<Tensor>& keep, bool copy = true)
 {
     const Tensor& x = in.x;
     const int64_t D = x.size(-1);
     mxl::ResidualNormParams p{};
-    const Rows xr = rows_of(x, D);
+    const Rows xr = rows_of(x, D, copy);
     keep.push_back(xr.t);
     p.x = xr.t.data_ptr(); p.ldx = xr.ld; p.x_bf16 = is_bf16(x);
     p.rows = xr.rows; p.cols = D;
     p.u_bf16 = p.x_bf16;
     p.branch = in.u.has_value();
     if (in.u) {
-        const Rows ur = rows_of(*in.u, D);
+        const Rows ur = rows_of(*in.u, D, copy);
         keep.push_back(ur.t);
         p.u = ur.t.data_ptr(); p.ldu = ur.ld; p.u_bf16 = is_bf16(*in.u);
     }
@@ -699,7 +699,7 @@ void check_norm_call(const NormInputs& in, const NormOptions& o, bool packed)
     TORCH_CHECK_VALUE(o.layer || (!in.pre_bias && !in.post_bias), "an RMS norm has no bias");
     if (in.x.numel() == 0) throw Status("mx_residual_norm_fwd", MX_ERR_SHAPE);
     std::vector<Tensor> keep;
-    mxl::ResidualNormParams p = norm_params(in, o, keep);
+    const mxl::ResidualNormParams p = norm_params(in, o, keep, false);
     check(mxl::check_residual_norm(p), "mx_residual_norm_fwd");
     if (packed && p.cols % 32 != 0) throw Status("mx_residual_norm_fwd", MX_ERR_SHAPE);
     TORCH_CHECK(in.x.is_cuda(), NORM, " runs on the GPU");
@@ -1038,7 +1038,7 @@ std::vector<Tensor> activation(const Tensor& p, bool silu, bool gated, bool eigh
     TORCH_CHECK_VALUE(p.dim() >= 1 && (!gated || p.size(-1) % 2 == 0), "a gated activation takes two halves of one length, got ", p.sizes());
     if (p.numel() == 0) throw Status("mx_activation_fwd", MX_ERR_SHAPE);
     {
-        const Rows r = rows_of(p, p.size(-1));
+        const Rows r = rows_of(p, p.size(-1), false);
         const mxl::ActivationParams a = act_params(r, is_bf16(p), silu, gated);
         check(mxl::check_activation(a, false), "mx_activation_fwd");
         if (packed && a.cols % 32 != 0) throw Status("mx_activation_fwd", MX_ERR_SHAPE);

@@ -231,3 +231,26 @@ def test_c_interface_refusals(mx):
     assert act("bwd", dp=0) == -1
     assert act(ac=FAKE) == -1 and act(ac=FAKE, as_=FAKE) == -4 and act(a=0, ac=FAKE, as_=FAKE, mode=5) == -4
     assert act(a=0, ac=FAKE + 8, as_=FAKE) == -5 and act(a=0, ac=FAKE, as_=FAKE, cols=48) == -2
+
+
+def test_workspace_of_sizes_that_no_call_takes(mx):
+    need = mx.binding.lib().mx_residual_norm_workspace_bytes
+    for rows, cols in ((1, 16385), (1, 1 << 20), (1, 1 << 40), (1 << 62, 64), (1 << 30, 64), ((1 << 63) - 1, 1), (-1, 64), (4, -64)):
+        assert need(rows, cols, 0) == 0 and need(rows, cols, 1) == 0, (rows, cols)
+    most = (1 << 35) - (1 << 19)                                          # elements of a call
+    for cols in (32, 16384):
+        assert need(most // cols + 1, cols, 0) == 0
+    for rows, cols in ((1, 1), (1, 16384), (most // 16384, 16384), (most // 32, 32)):
+        for gates in (0, 1, rows):
+            assert need(rows, cols, gates) > 0, (rows, cols, gates)
+
+
+def test_checkpoint_of_scattered_values_on_a_given_stream(mx):
+    """They would be gathered on the current stream."""
+    with pytest.raises(ValueError, match="stream"):
+        mx.mx_checkpoint_pack(torch.zeros(64, 4).t(), stream=1)
+    with pytest.raises(ValueError, match="stream"):
+        mx.mx_checkpoint_pack(torch.zeros(2, 4, 128)[:, :, :64], stream=1)
+    for values in (torch.zeros(4, 64), torch.zeros(4, 128)[:, :64], torch.zeros(2, 4, 64)):
+        with pytest.raises(RuntimeError, match="GPU"):
+            mx.mx_checkpoint_pack(values, stream=1)

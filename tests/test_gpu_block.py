@@ -595,6 +595,55 @@ def test_recorded_into_a_graph(mx):
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
 
 
+@pytest.mark.parametrize("d", [8192, 8200, 16384])
+def test_wide_rows_recorded_into_a_graph(mx, d):
+    torch.manual_seed(19)
+    x, u = (torch.randn((600, d), device="cuda").to(BF).requires_grad_(True) for _ in range(2))
+    w, v = (torch.randn(d, device="cuda").to(BF).requires_grad_(True) for _ in range(2))
+    gate = torch.randn((3, d), device="cuda").to(BF).requires_grad_(True)
+    dh, dy = (torch.randn((600, d), device="cuda").to(BF) for _ in range(2))
+
+    def step():
+        h, y = mx.residual_norm(x, u, pre_weight=w, post=True, post_weight=v, gate=gate, checkpoint=True)
+        return (h, y, *torch.autograd.grad((h, y), (x, u, w, v, gate), (dh, dy)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        recorded = step()
+    for k in range(3):
+        with torch.no_grad():
+            for t in (x, u, w, v, gate):
+                t.copy_(torch.randn_like(t))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.detach().clone() for t in recorded]
+        assert all(torch.equal(a, b) for a, b in zip(got, step())), k
+
+
+@pytest.mark.parametrize("d", [64, 8200])
+def test_c_interface_without_a_block_reads_no_scales(mx, d):
+    """u NULL: the norm of x alone, whatever stands in the scales; and its gradient."""
+    import ctypes
+    B = mx.binding
+    x, y, dy, dx = (torch.randn((5, d), device="cuda") for _ in range(4))
+    stats, w = torch.zeros((5, 4), device="cuda"), torch.randn(d, device="cuda")
+    need = B.lib().mx_residual_norm_workspace_bytes(5, d, 0)
+    work = torch.empty(need, device="cuda", dtype=torch.uint8)
+    results = []
+    for scale in (1.0, 0.0, float("nan")):
+        a = B.ResidualNormArgs(rows=5, cols=d, x=x.data_ptr(), y=y.data_ptr(), ldx=d, ldy=d, pre=1, pre_weight=w.data_ptr(), eps=1e-6,
+                               residual_scale=scale, branch_scale=scale, stats=stats.data_ptr())
+        st = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        assert B.lib().mx_residual_norm_fwd(ctypes.byref(a), st) == 0
+        b = B.ResidualNormGrads(branch=0, dy=dy.data_ptr(), dx=dx.data_ptr(), lddy=d, lddx=d, workspace=work.data_ptr(), workspace_bytes=need)
+        assert B.lib().mx_residual_norm_bwd(ctypes.byref(a), ctypes.byref(b), st) == 0
+        results.append((y.clone(), dx.clone()))
+    leaf = x.clone().requires_grad_(True)
+    want = mx.residual_norm(leaf, pre_weight=w)[1]
+    (dwant,) = torch.autograd.grad(want, leaf, dy)
+    for got in results:
+        assert torch.equal(got[0], want.detach()) and torch.equal(got[1], dwant)
+
+
 def test_two_graphs_and_a_side_stream(mx):
     """Calls on two streams at once and two recorded passes replayed together share no scratch memory."""
     torch.manual_seed(17)
