@@ -12,7 +12,7 @@ __device__ __forceinline__ uint32_t codes4(const F8& f, bool floor_mode, uint32_
 }
 
 // Mean (0 for RMS) and reciprocal deviation of the team's row; columns past the row's end hold zeros.
-template <int V, bool ANY, typename R>
+template <int V, bool TAIL, typename R>
 __device__ __forceinline__ float2 statistics(const R (&a)[V], Team& team, const NormArgs& g, const Place& at)
 {
     float mean = 0.0f;
@@ -32,11 +32,11 @@ __device__ __forceinline__ float2 statistics(const R (&a)[V], Team& team, const 
     for (int v = 0; v < V; ++v) {
         const int n = (int)g.cols - (int)at.col(v);
         // whole vectors lie in the row or behind it, where they are zero and stay it
-        const float m = ANY || v < V - 1 || n > 0 ? mean : 0.0f;
+        const float m = v < V - 1 || n > 0 ? mean : 0.0f;
         const F8 f = widen(a[v]);
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            const float d = !ANY || t < n ? f.v[t] - m : 0.0f;
+            const float d = !TAIL || v < V - 1 || t < n ? f.v[t] - m : 0.0f;
             q = __builtin_fmaf(d, d, q);
         }
     }
@@ -50,18 +50,19 @@ __device__ __forceinline__ float2 statistics(const R (&a)[V], Team& team, const 
 // vector a lane the parameters stay in registers, else they are read from LDS (four vectors: from cache).  Between the
 // loads of a row and its use the number of memory instructions is the same on every way through the loop (what there is
 // no array for goes to an empty descriptor), so that the wait for them is not one for all of the stores behind them too.
-template <typename XT, typename UT, int V, bool POST, bool GATE, bool EIGHT, bool ANY>
+template <typename XT, typename UT, int V, bool POST, bool GATE, bool EIGHT, RowEnd END>
 __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const NormArgs g)
 {
     extern __shared__ float lds[];                                       // the parameters, where a lane has two or three vectors
     __shared__ TeamScratch scratch;
+    constexpr bool TAIL = END != ROW_WHOLE;
     using Params = ParamLds<POST, GATE, true, false>;
     const uint32_t stride = g.layer ? Params::STRIDE : ParamLds<POST, GATE, false, false>::STRIDE;      // the biases come last
     const uint32_t team_in_block = threadIdx.x / g.lanes, lane = threadIdx.x % g.lanes;
     const uint32_t teams = blockDim.x / g.lanes;
     Team team{g.lanes, team_in_block * (g.lanes >> 6), &scratch};
     const uint32_t step = g.lanes * 8u, vectors = g.lanes * V;
-    const bool post = POST && (!ANY || g.post), gated = GATE && (!ANY || g.gate != nullptr), gate_by_row = GATE && g.gate_by_row;
+    const bool post = POST && (!TAIL || g.post), gated = GATE && (!TAIL || g.gate != nullptr), gate_by_row = GATE && g.gate_by_row;
 
     // every g.teams-th row, so that the chip works in one window of the matrix at a time; with gate rows a run of rows, so that a
     // team's gate row rarely changes
@@ -69,14 +70,14 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
     const bool runs = GATE && g.row_step == 1;
     const int64_t first = runs ? g.rows * k0 / g.teams : k0, begin = k >= g.teams ? first : runs ? g.rows * k / g.teams : k;
     const uint32_t count = k >= g.teams ? 0u : (uint32_t)(runs ? g.rows * (k + 1) / g.teams - begin : (g.rows - k + g.teams - 1) / g.teams);
-    Place at{first, (uint32_t)(begin - first), lane * 8u, step, g.cols, g.pitch8, count > 0};
+    Place at{first, (uint32_t)(begin - first), lane * 8u, step, g.cols, g.pitch8, count > 0, back_of<END, V>(g.cols, lane * 8u, step)};
     Raw<XT> xn[V];
     Raw<UT> un[V];
     auto fetch = [&](const Place& at) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            xn[v] = load_vec<ANY, V, XT>(g.x, g.ldx, at, v);
-            un[v] = load_vec<ANY, V, UT>(g.u, g.ldu, at, v);
+            xn[v] = load_vec<END, V, XT>(g.x, g.ldx, at, v);
+            un[v] = load_vec<END, V, UT>(g.u, g.ldu, at, v);
         }
     };
     fetch(at);
@@ -89,17 +90,17 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
         if (GATE && !gate_by_row) f(P_GATE);
     };
     if constexpr (V == 1) {
-        each_param([&](NormParam which) { held[which] = norm_param<ANY>(g, which, at.col0); });
+        each_param([&](NormParam which) { held[which] = norm_param<TAIL>(g, which, at.col0); });
     } else if constexpr (V < 4) {
         each_param([&](NormParam which) {
-            for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x) Params::put(lds, stride, which, c, norm_param<ANY>(g, which, c * 8));
+            for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x) Params::put(lds, stride, which, c, norm_param<TAIL>(g, which, c * 8));
         });
         __syncthreads();
     } else {
         each_param([&](NormParam which) {
             if (g.plane[which] == ParamPlanes::NO_PLANE) return;
             for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x)
-                ParamPlanes::put(lds, g.plane[which], vectors, c, param_is_bf16(g, which), norm_param<ANY>(g, which, c * 8));
+                ParamPlanes::put(lds, g.plane[which], vectors, c, param_is_bf16(g, which), norm_param<TAIL>(g, which, c * 8));
         });
         __syncthreads();
     }
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
         in_run = at.row() - gate_row * g.gate_run;
     }
     float* own_gate = lds + vectors * stride + team_in_block * vectors * Params::GATE_STRIDE;     // a lane reads what it wrote
-    auto gate_of_row = [&](int v) { return param8<ANY>(g.gate, g.gate_bf16, gate_row * g.ld_gate + at.col(v), at.left(v), 0.0f); };
+    auto gate_of_row = [&](int v) { return param8<TAIL>(g.gate, g.gate_bf16, gate_row * g.ld_gate + at.col(v), at.left(v), 0.0f); };
     auto take_gate = [&]() {
         if constexpr (V == 1) held[P_GATE] = gate_of_row(0);
         else if constexpr (V < 4) {
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
         } else {
             if (which == P_GATE && gate_by_row) return gate_of_row(v);
             if (g.plane[which] != ParamPlanes::NO_PLANE) return ParamPlanes::get(lds, g.plane[which], vectors, lane + v * g.lanes, param_is_bf16(g, which));
-            return norm_param<ANY>(g, which, at.col(v));
+            return norm_param<TAIL>(g, which, at.col(v));
         }
     };
 
@@ -139,13 +140,15 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
             h[v] = xn[v];
             u[v] = un[v];
         }
+        settle(u[V - 1], at.back);
+        settle(h[V - 1], at.back);
         forget();
         Place next = at;
         next.first += g.row_step;
         next.live = i + 1 < count;
         fetch(next);
         float2 su = make_float2(0.0f, 0.0f);
-        if (post) su = statistics<V, ANY>(u, team, g, at);
+        if (post) su = statistics<V, TAIL>(u, team, g, at);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             renew(u[v]);
@@ -172,11 +175,11 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
             for (int t = 0; t < 8; ++t) b.v[t] = g.rho * x.v[t] + g.sigma * b.v[t];
             narrow(b, h[v]);
             b = widen(h[v]);                                             // the stream as it is stored
-            store_vec<ANY, V, XT>(g.h, g.ldh, at, v, b);
+            store_vec<END, V, XT>(g.h, g.ldh, at, v, b);
             if (EIGHT) store_codes8<V>(g.h8, g.h8_scales, at, v, b);
             if (V > 1) __builtin_amdgcn_sched_barrier(0);                // one vector at a time: registers are short
         }
-        const float2 sh = statistics<V, ANY>(h, team, g, at);
+        const float2 sh = statistics<V, TAIL>(h, team, g, at);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             renew(h[v]);
@@ -201,7 +204,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
                 __builtin_amdgcn_raw_buffer_store_b8((uint8_t)byte, descriptor(g.y_scales, at.first * groups),
                                                      in && (lane & 3u) == 0 ? at.behind * groups + (at.col0 >> 5) : OFF_END, v * step >> 5, 0);
             } else {
-                store_vec<ANY, V, UT>(g.y, g.ldy, at, v, y);
+                store_vec<END, V, UT>(g.y, g.ldy, at, v, y);
             }
             if (V > 1) __builtin_amdgcn_sched_barrier(0);
         }
@@ -297,10 +300,11 @@ hipError_t launch_fwd(const ResidualNormParams& p, hipStream_t st)
     const bool gate_rows = p.gate != nullptr && p.gate_rows > 1;
     NormArgs g;
     uint32_t teams, grid;
-    bool any;
+    const RowEnd end = row_end(p.cols);
+    bool far = false;
     size_t lds;
     for (;;) {
-        const uint32_t most = std::max(1u, NORM_THREADS / s.lanes);
+        const uint32_t most = far ? 1 : std::max(1u, NORM_THREADS / s.lanes);
         teams = whole_waves((uint32_t)std::min<int64_t>(most, std::max<int64_t>(1, (p.rows + UNITS - 1) / UNITS)), s.lanes);
         g = norm_args(p, s);
         // 8 waves on a unit, with one vector a lane 16; more of them, or smaller workgroups, leave less of the memory's rate
@@ -310,25 +314,29 @@ hipError_t launch_fwd(const ResidualNormParams& p, hipStream_t st)
         g.team_rows = (p.rows + g.teams - 1) / g.teams;
         g.row_step = gate_rows ? 1 : g.teams;
         const int64_t span = (teams + 1) * (gate_rows ? g.team_rows : 1);                // rows that a workgroup's teams reach over
-        any = p.cols % 8 != 0 || !by_descriptor(p.x, p.x_bf16, p.ldx, span) || !by_descriptor(p.u, p.u_bf16, p.ldu, span) ||
-              !by_descriptor(p.h, p.x_bf16, p.ldh, span) || !by_descriptor(p.y, p.u_bf16, p.ldy, span);
+        if (!far && (!covers(p.x, p.x_bf16, p.ldx, span) || !covers(p.u, p.u_bf16, p.ldu, span) || !covers(p.h, p.x_bf16, p.ldh, span) ||
+                     !covers(p.y, p.u_bf16, p.ldy, span))) {
+            far = true;
+            s = one_team(s, p.cols);
+            continue;
+        }
         lds = s.v == 1 ? 0 :
               s.v == 4 ? give_planes(g, s, {{P_PRE_WEIGHT, p.y || p.y_codes}, {P_POST_WEIGHT, p.post}, {P_GATE, p.gate && !gate_rows},
                                             {P_PRE_BIAS, p.layer && (p.y || p.y_codes)}, {P_POST_BIAS, p.layer && p.post}}) :
-                         param_bytes(s, any, p.post, p.gate != nullptr, p.layer, false, gate_rows ? teams : 0);
+                         param_bytes(s, end, p.post, p.gate != nullptr, p.layer, false, gate_rows ? teams : 0);
         if (lds <= NORM_LDS_MAX) break;
         s = four_vectors(p.cols);
     }
     const uint32_t threads = teams * s.lanes;
     hipError_t e = hipSuccess;
     by_vectors(s.v, [&](auto v) {
-        by_kind(any, p.post, p.gate != nullptr, [&](auto post, auto gate, auto odd) {
+        by_kind(end, p.post, p.gate != nullptr, [&](auto post, auto gate, auto ends) {
             auto run = [&](auto eight) {
-                e = start_norm(residual_norm_fwd_kernel<XT, UT, decltype(v)::value, decltype(post)::value, decltype(gate)::value,
-                                                        decltype(eight)::value, decltype(odd)::value>, grid, threads, lds, st, g);
+                if constexpr (decltype(ends)::value != ROW_SHORT || decltype(v)::value == 1) e = start_norm(residual_norm_fwd_kernel<XT, UT, decltype(v)::value, decltype(post)::value, decltype(gate)::value,
+                                                        decltype(eight)::value, decltype(ends)::value>, grid, threads, lds, st, g);
             };
-            if constexpr (decltype(odd)::value) run(std::true_type{});
-            else                                by_flag(p.h8 != nullptr || p.u8 != nullptr, run);
+            if constexpr (decltype(ends)::value != ROW_WHOLE) run(std::true_type{});
+            else                                              by_flag(p.h8 != nullptr || p.u8 != nullptr, run);
         });
     });
     return e;
@@ -342,14 +350,19 @@ struct BwdPlan {
     bool halves;                             // rows first, then sums (strips of columns, a wave each)
 };
 
-BwdPlan plan_bwd(int64_t rows, int64_t cols, int64_t gate_rows)
+// far_grid: the workgroups of a launch whose teams are one each (one_team), which takes no more workspace than the other; 0: not so.
+BwdPlan plan_bwd(int64_t rows, int64_t cols, int64_t gate_rows, uint32_t far_grid = 0)
 {
     BwdPlan b{};
     b.shape = shape_for(cols, 2);
-    b.halves = b.shape.v == 4;
+    // also where the parameters of the largest kind and the teams' gate rows do not fit in LDS
+    b.halves = b.shape.v == 4 || (gate_rows > 1 && param_bytes(b.shape, ROW_WHOLE, true, true, true, true,
+                                                               whole_waves(NORM_THREADS / b.shape.lanes, b.shape.lanes)) > NORM_LDS_MAX);
     if (b.halves) b.shape = {64, 1};
     b.strips = b.halves ? (uint32_t)((cols + 511) / 512) : 1;
-    const uint32_t lanes = b.shape.lanes, most = NORM_THREADS / lanes, grid = UNITS / b.strips;      // 8 waves on a unit: few sums to add up
+    if (far_grid > 0) b.shape = one_team(b.shape, cols);
+    const uint32_t lanes = b.shape.lanes, most = far_grid > 0 ? 1 : NORM_THREADS / lanes;
+    const uint32_t grid = far_grid > 0 ? far_grid : UNITS / b.strips;                      // 8 waves on a unit: few sums to add up
     b.teams_per_block = (uint32_t)std::min<int64_t>(most, std::max<int64_t>(1, (rows + grid - 1) / grid));
     b.teams_per_block = whole_waves(b.teams_per_block, lanes);
     const int64_t teams = std::min<int64_t>(rows, (int64_t)grid * b.teams_per_block), run = rows / gate_rows;
@@ -358,7 +371,7 @@ BwdPlan plan_bwd(int64_t rows, int64_t cols, int64_t gate_rows)
         b.teams = gate_rows * b.pieces;
         b.team_rows = (run + b.pieces - 1) / b.pieces;
     } else {
-        b.teams = gate_rows <= 2 * teams ? gate_rows : teams;
+        b.teams = gate_rows <= 2 * teams && far_grid == 0 ? gate_rows : teams;
         b.team_rows = (gate_rows + b.teams - 1) / b.teams * run;
     }
     b.grid = (uint32_t)((b.teams + b.teams_per_block - 1) / b.teams_per_block);
@@ -385,11 +398,12 @@ hipError_t launch_residual_norm_bwd(const ResidualNormParams& p, const ResidualN
 {
     const int64_t gate_rows = p.gate != nullptr ? p.gate_rows : 1;
     const bool eight = p.h8 != nullptr || p.u8 != nullptr;
-    const BwdPlan b = plan_bwd(p.rows, p.cols, gate_rows);
+    BwdPlan b = plan_bwd(p.rows, p.cols, gate_rows);
     const int64_t span = (b.teams_per_block + 1) * (gate_rows > 1 ? b.team_rows : 1);      // rows that a workgroup's teams reach over
-    const bool any = p.cols % 8 != 0 || !by_descriptor(d.dh, p.x_bf16, d.lddh, span) || !by_descriptor(d.dy, p.u_bf16, d.lddy, span) ||
-                     !by_descriptor(d.dx, p.x_bf16, d.lddx, span) || !by_descriptor(d.du, p.u_bf16, d.lddu, span) ||
-                     (!eight && (!by_descriptor(p.h, p.x_bf16, p.ldh, span) || !by_descriptor(p.u, p.u_bf16, p.ldu, span)));
+    if (!covers(d.dh, p.x_bf16, d.lddh, span) || !covers(d.dy, p.u_bf16, d.lddy, span) || !covers(d.dx, p.x_bf16, d.lddx, span) ||
+        !covers(d.du, p.u_bf16, d.lddu, span) || (!eight && (!covers(p.h, p.x_bf16, p.ldh, span) || !covers(p.u, p.u_bf16, p.ldu, span))))
+        b = plan_bwd(p.rows, p.cols, gate_rows, b.grid);
+    const RowEnd end = row_end(p.cols);
     const auto launch = p.layer ? launch_norm_bwd_layer : launch_norm_bwd_rms;
     NormGradArgs a{};
     a.f = norm_args(p, b.shape);
@@ -421,17 +435,15 @@ hipError_t launch_residual_norm_bwd(const ResidualNormParams& p, const ResidualN
         r.f.teams = r.f.row_step = grid;
         r.f.team_rows = (p.rows + grid - 1) / grid;
         const size_t lds = give_planes(r.f, s, {{P_PRE_WEIGHT, d.dy != nullptr}, {P_POST_WEIGHT, p.post}, {P_GATE, p.gate && gate_rows == 1}});
-        e = launch(r, p.x_bf16, p.u_bf16, eight, any, s.v, BWD_ROWS, grid, s.lanes, lds, st);
+        e = launch(r, p.x_bf16, p.u_bf16, eight, end, s.v, BWD_ROWS, grid, s.lanes, lds, st);
         if (e != hipSuccess || (!wanted && !a.want_gate)) return e;
     }
     a.f.teams = b.teams; a.f.team_rows = b.team_rows; a.f.row_step = gate_rows > 1 ? 1 : b.teams;
     const uint32_t threads = b.teams_per_block * b.shape.lanes, width = b.shape.lanes * b.shape.v * 8;
-    // the parameters, with the teams' gate rows where there is room for them; at the end the sums
-    auto bytes = [&](uint32_t own) { return param_bytes(b.shape, any, p.post, p.gate != nullptr, p.layer, true, own); };
-    a.f.gate_in_lds = a.f.gate_by_row && bytes(b.teams_per_block) <= NORM_LDS_MAX;
-    size_t lds = bytes(a.f.gate_in_lds ? b.teams_per_block : 0);
+    // the parameters, with the teams' gate rows; at the end the sums
+    size_t lds = param_bytes(b.shape, end, p.post, p.gate != nullptr, p.layer, true, a.f.gate_by_row ? b.teams_per_block : 0);
     if (b.teams_per_block > 1) lds = std::max(lds, (size_t)b.teams_per_block * width * sizeof(float));
-    e = launch(a, p.x_bf16, p.u_bf16, eight, any, b.shape.v, b.halves ? BWD_SUMS : BWD_ALL, dim3(b.grid, b.strips), threads, lds, st);
+    e = launch(a, p.x_bf16, p.u_bf16, eight, end, b.shape.v, b.halves ? BWD_SUMS : BWD_ALL, dim3(b.grid, b.strips), threads, lds, st);
     if (e != hipSuccess || !wanted) return e;
     residual_norm_finish_kernel<<<(uint32_t)((p.cols + 31) / 32) * (SUMS - 1 + gates), 32 * FINISH_RUNS, 0, st>>>(f);
     return hipGetLastError();

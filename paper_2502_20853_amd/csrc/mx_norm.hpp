@@ -45,7 +45,6 @@ struct NormArgs {
     float inv_cols, rho, sigma, eps;
     uint8_t plane[8];                                         // of the parameters in LDS (ParamPlanes)
     bool layer, post, param_bf16, gate_bf16, gate_by_row, floor_mode;
-    bool gate_in_lds;                                         // the teams' gate rows
 };
 
 struct NormGradArgs {
@@ -151,11 +150,14 @@ __device__ __forceinline__ F8 norm_param(const NormArgs& g, int which, uint32_t 
 }
 
 // ---- a team's rows of a matrix ---------------------------------------------------------------------
-// ANY: rows of any length and alignment, by address.  Else (a length of whole vectors, 16-byte rows) through a buffer
-// descriptor that starts at a row which is the same for the whole workgroup: the descriptor moves on by scalar instructions, a
-// lane's offset from there never changes, and a lane without work has one beyond the descriptor's end, where the hardware
-// returns zero and drops stores.  That saves the address arithmetic and its registers, and every branch.
-// A matrix that there is not (null) reads as zero and takes no stores.
+// Rows at any alignment, through a buffer descriptor that starts at a row which is the same for the whole workgroup: the
+// descriptor moves on by scalar instructions, a lane's offset from there never changes, and a lane without work has one beyond
+// the descriptor's end, where the hardware returns zero and drops stores.  That saves the address arithmetic and its registers,
+// and every branch.  A matrix that there is not (null) reads as zero and takes no stores.
+// How a row ends: with whole vectors; inside one (ROW_ENDS: its lane loads the row's last eight elements and moves them down,
+// and stores what it has in three pieces; nothing of that is a branch around a load, which would be waited for at once: 9850 rows
+// of 1001 in bf16 take 32.7 us with one, 28.3 with all rows by address); or in its first vector (ROW_SHORT: by address).
+enum RowEnd { ROW_WHOLE, ROW_ENDS, ROW_SHORT };
 constexpr uint32_t OFF_END = 0x80000000u;                // beyond the end of every descriptor
 constexpr int64_t OFF_MAX = 0x7FFFFFF0;                  // what one covers: a workgroup's rows have to fit
 
@@ -201,6 +203,7 @@ struct Place {
     uint32_t col0, step;     // the lane's first column, columns from one of its vectors to the next
     uint32_t cols, pitch8;
     uint32_t live;           // whether the team has a row
+    uint32_t back;           // by how much the lane's last vector begins before its column (ROW_ENDS)
     __device__ __forceinline__ int64_t row() const { return first + behind; }
     __device__ __forceinline__ uint32_t col(int v) const { return col0 + v * step; }
     __device__ __forceinline__ int left(int v) const { return live != 0 ? (int)cols - (int)col(v) : 0; }
@@ -208,25 +211,82 @@ struct Place {
     template <int V> __device__ __forceinline__ bool in(int v, uint32_t end) const { return live != 0 && (v < V - 1 || col(v) < end); }
 };
 
-template <bool ANY, int V, typename T>
-__device__ __forceinline__ Raw<T> load_vec(const void* base, int64_t ld, const Place& at, int v)
+template <RowEnd END, int V>
+__device__ __forceinline__ uint32_t back_of(uint32_t cols, uint32_t col0, uint32_t step)
 {
-    if constexpr (ANY) return load_raw<true>(static_cast<const T*>(base) + at.row() * ld + at.col(v), base == nullptr ? 0 : at.left(v));
-    const uint32_t off = (at.behind * (uint32_t)ld + at.col0) * sizeof(T);
-    return buffer_load_raw(descriptor(base, at.first * ld * (int64_t)sizeof(T)), at.in<V>(v, at.cols) ? off : OFF_END, v * at.step * sizeof(T), T{});
+    const int n = left(cols, col0 + (V - 1) * step);
+    return END == ROW_ENDS && n > 0 && n < 8 ? 8u - n : 0u;
 }
 
-template <bool ANY, int V, typename T>
+template <RowEnd END, int V, typename T>
+__device__ __forceinline__ Raw<T> load_vec(const void* base, int64_t ld, const Place& at, int v)
+{
+    if constexpr (END == ROW_SHORT) return load_raw<true>(static_cast<const T*>(base) + at.row() * ld + at.col(v), base == nullptr ? 0 : at.left(v));
+    const __amdgpu_buffer_rsrc_t r = descriptor(base, at.first * ld * (int64_t)sizeof(T));
+    const bool in = at.in<V>(v, at.cols);
+    if (END == ROW_ENDS && v == V - 1) return buffer_load_raw(r, in ? (at.behind * (uint32_t)ld + at.col(v) - at.back) * sizeof(T) : OFF_END, 0, T{});
+    return buffer_load_raw(r, in ? (at.behind * (uint32_t)ld + at.col0) * sizeof(T) : OFF_END, v * at.step * sizeof(T), T{});
+}
+
+// What load_vec gave for a lane's last vector, moved down to where it belongs; zeros come in behind it.
+__device__ __forceinline__ void settle(RawBf16& r, uint32_t back)
+{
+    if (back == 0) return;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = back & 1 ? __builtin_amdgcn_alignbit(i < 3 ? r.w[i + 1] : 0u, r.w[i], 16) : r.w[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = back & 2 ? (i < 3 ? w[i + 1] : 0u) : w[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = back & 4 ? (i < 2 ? w[i + 2] : 0u) : w[i];
+}
+__device__ __forceinline__ void settle(F8& r, uint32_t back)
+{
+    if (back == 0) return;
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = back & 1 ? (i < 7 ? r.v[i + 1] : 0.0f) : r.v[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = back & 2 ? (i < 6 ? w[i + 2] : 0.0f) : w[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.v[i] = back & 4 ? (i < 4 ? w[i + 4] : 0.0f) : w[i];
+}
+
+// The first n of eight elements, n < 8 (others: none), in pieces of four, two and one.
+__device__ __forceinline__ void buffer_store_end(__amdgpu_buffer_rsrc_t r, uint32_t off, const RawBf16& v, int n)
+{
+    const bool some = n > 0 && n < 8, four = n & 4, two = n & 2;
+    const uint32_t a = four ? v.w[2] : v.w[0], b = four ? v.w[3] : v.w[1];
+    __builtin_amdgcn_raw_buffer_store_b64(u2_vec{v.w[0], v.w[1]}, r, some && four ? off : OFF_END, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b32(a, r, some && two ? off + (n & 4) * 2u : OFF_END, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(two ? b : a), r, some && (n & 1) ? off + (n & 6) * 2u : OFF_END, 0, 0);
+}
+__device__ __forceinline__ void buffer_store_end(__amdgpu_buffer_rsrc_t r, uint32_t off, const F8& v, int n)
+{
+    const bool some = n > 0 && n < 8, four = n & 4, two = n & 2;
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v.v[i]);
+    const uint32_t a = four ? w[4] : w[0], b = four ? w[5] : w[1], c = four ? w[6] : w[2];
+    __builtin_amdgcn_raw_buffer_store_b128(u4_vec{w[0], w[1], w[2], w[3]}, r, some && four ? off : OFF_END, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b64(u2_vec{a, b}, r, some && two ? off + (n & 4) * 4u : OFF_END, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b32(two ? c : a, r, some && (n & 1) ? off + (n & 6) * 4u : OFF_END, 0, 0);
+}
+
+template <RowEnd END, int V, typename T>
 __device__ __forceinline__ void store_vec(void* base, int64_t ld, const Place& at, int v, const F8& f)
 {
     Raw<T> raw;
     narrow(f, raw);
-    if constexpr (ANY) {
+    if constexpr (END == ROW_SHORT) {
         store_raw<true>(static_cast<T*>(base) + at.row() * ld + at.col(v), raw, base == nullptr ? 0 : at.left(v));
         return;
     }
-    const uint32_t off = (at.behind * (uint32_t)ld + at.col0) * sizeof(T);
-    buffer_store_raw(descriptor(base, at.first * ld * (int64_t)sizeof(T)), at.in<V>(v, at.cols) ? off : OFF_END, v * at.step * sizeof(T), raw);
+    const __amdgpu_buffer_rsrc_t r = descriptor(base, at.first * ld * (int64_t)sizeof(T));
+    const uint32_t off = (at.behind * (uint32_t)ld + at.col0) * sizeof(T), step = v * at.step * sizeof(T);
+    const bool ends = END == ROW_ENDS && v == V - 1;
+    buffer_store_raw(r, (ends ? at.left(v) >= 8 : at.in<V>(v, at.cols)) ? off : OFF_END, step, raw);
+    if (ends) buffer_store_end(r, off + step, raw, at.left(v));
 }
 
 // 8-bit codes and scale bytes; their rows are whole groups, so they always go through descriptors.
@@ -312,19 +372,21 @@ void by_types(bool x_bf16, bool u_bf16, F&& f)
     else f(float{}, float{});
 }
 
-// Calls f with a truth value, with what a kernel is compiled for (post-norm, gate, rows of any kind), or with a number of
-// vectors, as types.
+// Calls f with a truth value, with what a kernel is compiled for (post-norm, gate, how rows end), or with a number of vectors, as types.
 template <typename F>
 void by_flag(bool a, F&& f) { a ? f(std::true_type{}) : f(std::false_type{}); }
+inline RowEnd row_end(int64_t cols) { return cols < 8 ? ROW_SHORT : cols % 8 != 0 ? ROW_ENDS : ROW_WHOLE; }
+template <RowEnd END> using Ends = std::integral_constant<RowEnd, END>;
 template <typename F>
-void by_kind(bool any, bool post, bool gate, F&& f)
+void by_kind(RowEnd end, bool post, bool gate, F&& f)
 {
     using Y = std::true_type;
     using N = std::false_type;
-    // rows of any length and alignment have one kernel for all kinds
-    if (any)       f(Y{}, Y{}, Y{});
-    else if (post) gate ? f(Y{}, Y{}, N{}) : f(Y{}, N{}, N{});
-    else           gate ? f(N{}, Y{}, N{}) : f(N{}, N{}, N{});
+    // rows that do not end with a whole vector have one kernel for all kinds
+    if (end == ROW_SHORT)     f(Y{}, Y{}, Ends<ROW_SHORT>{});
+    else if (end == ROW_ENDS) f(Y{}, Y{}, Ends<ROW_ENDS>{});
+    else if (post)            gate ? f(Y{}, Y{}, Ends<ROW_WHOLE>{}) : f(Y{}, N{}, Ends<ROW_WHOLE>{});
+    else                      gate ? f(N{}, Y{}, Ends<ROW_WHOLE>{}) : f(N{}, N{}, Ends<ROW_WHOLE>{});
 }
 template <typename F>
 void by_vectors(int v, F&& f)
@@ -335,18 +397,20 @@ void by_vectors(int v, F&& f)
     else             f(std::integral_constant<int, 4>{});
 }
 
-// Whether a matrix's rows go through descriptors: `rows` of them from a workgroup's first one on.
-inline bool by_descriptor(const void* p, bool bf16, int64_t ld, int64_t rows)
+// Whether one descriptor covers so many rows of a matrix.
+inline bool covers(const void* p, bool bf16, int64_t ld, int64_t rows)
 {
-    const int64_t bytes = bf16 ? 2 : 4;
-    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * bytes % 16 == 0 && rows <= OFF_MAX / bytes / std::max<int64_t>(1, ld) - 1;
+    return p == nullptr || rows <= OFF_MAX / (bf16 ? 2 : 4) / std::max<int64_t>(1, ld) - 1;
 }
 
+// Where rows lie so far apart that one does not cover those of a workgroup, each team is a workgroup of its own.
+inline TeamShape one_team(const TeamShape& s, int64_t cols) { return s.lanes >= 64 ? s : TeamShape{64, (int)((cols + 511) / 512)}; }
+
 // Bytes of LDS that the parameters of a kernel take (the ParamLds of its kind), and gate rows of the teams' own.
-inline size_t param_bytes(const TeamShape& s, bool any, bool post, bool gate, bool layer, bool backward, uint32_t own_gates)
+inline size_t param_bytes(const TeamShape& s, RowEnd end, bool post, bool gate, bool layer, bool backward, uint32_t own_gates)
 {
     size_t words = 0;
-    by_kind(any, post, gate, [&](auto p, auto g, auto) {
+    by_kind(end, post, gate, [&](auto p, auto g, auto) {
         by_flag(layer, [&](auto l) {
             by_flag(backward, [&](auto b) { words = ParamLds<decltype(p)::value, decltype(g)::value, decltype(l)::value, decltype(b)::value>::STRIDE; });
         });
@@ -382,7 +446,7 @@ hipError_t start_norm(K kernel, dim3 grid, uint32_t threads, size_t lds, hipStre
 }
 
 // The backward kernels by norm (a file each).
-hipError_t launch_norm_bwd_rms(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, BwdPart part, dim3 grid, uint32_t threads, size_t lds, hipStream_t st);
-hipError_t launch_norm_bwd_layer(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, BwdPart part, dim3 grid, uint32_t threads, size_t lds, hipStream_t st);
+hipError_t launch_norm_bwd_rms(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, RowEnd end, int v, BwdPart part, dim3 grid, uint32_t threads, size_t lds, hipStream_t st);
+hipError_t launch_norm_bwd_layer(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, RowEnd end, int v, BwdPart part, dim3 grid, uint32_t threads, size_t lds, hipStream_t st);
 
 }  // namespace mxl

@@ -8,14 +8,16 @@ namespace mxl {
 template <typename T, bool CKPT> struct Kept { Raw<T> raw; };
 template <typename T> struct Kept<T, true> { Codes8 codes; uint32_t byte; };
 
-template <bool ANY, int V, typename T, bool CKPT>
+template <RowEnd END, int V, typename T, bool CKPT>
 __device__ __forceinline__ void load_kept(Kept<T, CKPT>& k, const void* p, int64_t ld, const uint8_t* codes, const uint8_t* scales, const Place& at, int v)
 {
     if constexpr (CKPT) k.codes = load_codes8<V>(codes, scales, at, v, k.byte);
-    else                k.raw = load_vec<ANY, V, T>(p, ld, at, v);
+    else                k.raw = load_vec<END, V, T>(p, ld, at, v);
 }
 template <typename T> __device__ __forceinline__ F8 value_of(const Kept<T, true>& k) { return unpack8(k.codes, k.byte); }
 template <typename T> __device__ __forceinline__ F8 value_of(const Kept<T, false>& k) { return widen(k.raw); }
+template <typename T> __device__ __forceinline__ void settle(Kept<T, true>&, uint32_t) {}         // codes lie in whole vectors
+template <typename T> __device__ __forceinline__ void settle(Kept<T, false>& k, uint32_t back) { settle(k.raw, back); }
 template <typename T> __device__ __forceinline__ void renew(Kept<T, true>& k) { renew(k.codes); }
 template <typename T> __device__ __forceinline__ void renew(Kept<T, false>& k) { renew(k.raw); }
 
@@ -29,13 +31,13 @@ struct RowPlan {
     RowMode mode;
     bool keep;
 };
-template <typename XT, typename UT, int V, bool POST, bool GATE, bool LAYER, bool CKPT, BwdPart PART>
+template <typename XT, typename UT, int V, bool POST, bool GATE, bool LAYER, bool CKPT, bool TAIL, BwdPart PART>
 constexpr RowPlan row_plan()
 {
     constexpr int x = sizeof(XT) * 2, u = sizeof(UT) * 2;               // registers of eight values
     constexpr int sums = PART == BWD_ROWS ? 0 : (LAYER ? 2 : 1) * (POST ? 2 : 1) + GATE;
     constexpr int raw = u + x + (CKPT ? 3 : x) + (!POST && !GATE ? 0 : CKPT ? 3 : u);
-    constexpr int fixed = V * 8 * sums + 76, kept = POST ? V * 8 : 0;
+    constexpr int fixed = V * 8 * sums + 76 + (TAIL ? 24 : 0), kept = POST ? V * 8 : 0;
     if (fixed + kept + 2 * V * raw <= 240) return {ROW_AHEAD, true};
     if (fixed + kept + V * raw <= 240) return {ROW_HELD, true};
     return {fixed + V * raw <= 240 ? ROW_HELD : ROW_AGAIN, false};
@@ -48,7 +50,7 @@ constexpr RowPlan row_plan()
 // Up to nine FP32 vectors of the row's length would live in registers: the sums do, the parameters are read from LDS
 // (with four vectors a lane from cache), and what a row needs again behind its sums is kept as loaded.  What is missing (a
 // gradient, a weight) reads as zero or one, so that the loop has next to no branches.
-template <typename XT, typename UT, int V, bool POST, bool GATE, bool LAYER, bool CKPT, bool ANY, BwdPart PART>
+template <typename XT, typename UT, int V, bool POST, bool GATE, bool LAYER, bool CKPT, RowEnd END, BwdPart PART>
 __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const NormGradArgs a)
 {
     extern __shared__ float lds[];               // the parameters; at the end [teams][width] for the sums
@@ -59,8 +61,8 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
     Team team{g.lanes, team_in_block * (g.lanes >> 6), &scratch};
     const uint32_t step = g.lanes * 8u, width = step * V, vectors = g.lanes * V;
     const uint32_t base = PART == BWD_SUMS ? blockIdx.y * width : 0u, col0 = base + lane * 8u;           // of the strip
-    constexpr bool READ_U = POST || GATE;
-    const bool post = POST && (!ANY || g.post), gate_by_row = GATE && g.gate_by_row;
+    constexpr bool READ_U = POST || GATE, TAIL = END != ROW_WHOLE;
+    const bool post = POST && (!TAIL || g.post), gate_by_row = GATE && g.gate_by_row;
 
     const int64_t k0 = (int64_t)blockIdx.x * teams, k = k0 + team_in_block;
     // without gate rows every g.teams-th row, as in the forward pass
@@ -76,7 +78,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
     using Params = ParamLds<POST, GATE, LAYER, true>;
     if constexpr (PART != BWD_ROWS) {
         auto fill = [&](NormParam which) {
-            for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x) Params::put(lds, Params::STRIDE, which, c, norm_param<ANY>(g, which, base + c * 8));
+            for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x) Params::put(lds, Params::STRIDE, which, c, norm_param<TAIL>(g, which, base + c * 8));
         };
         fill(P_PRE_WEIGHT);
         if (POST) fill(P_POST_WEIGHT);
@@ -87,7 +89,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
         auto fill = [&](NormParam which) {
             if (g.plane[which] == ParamPlanes::NO_PLANE) return;
             for (uint32_t c = threadIdx.x; c < vectors; c += blockDim.x)
-                ParamPlanes::put(lds, g.plane[which], vectors, c, param_is_bf16(g, which), norm_param<ANY>(g, which, c * 8));
+                ParamPlanes::put(lds, g.plane[which], vectors, c, param_is_bf16(g, which), norm_param<TAIL>(g, which, c * 8));
         };
         fill(P_PRE_WEIGHT);
         if (POST) fill(P_POST_WEIGHT);
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[s][v] = mxd::zero8();
 
-    constexpr RowPlan PLAN = row_plan<XT, UT, V, POST, GATE, LAYER, CKPT, PART>();
+    constexpr RowPlan PLAN = row_plan<XT, UT, V, POST, GATE, LAYER, CKPT, TAIL, PART>();
     constexpr RowMode MODE = PLAN.mode;
     struct Vec {                                                         // a lane's part of a row, as loaded
         Raw<UT> dy;
@@ -111,12 +113,12 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
     };
     auto load = [&](Vec& r, const Place& at, int v, bool h, bool u) {
         if (h) {
-            r.dy = load_vec<ANY, V, UT>(a.dy, a.lddy, at, v);
-            load_kept<ANY, V, XT, CKPT>(r.h, g.h, g.ldh, g.h8, g.h8_scales, at, v);
+            r.dy = load_vec<END, V, UT>(a.dy, a.lddy, at, v);
+            load_kept<END, V, XT, CKPT>(r.h, g.h, g.ldh, g.h8, g.h8_scales, at, v);
         }
         if (u) {
-            r.dh = load_vec<ANY, V, XT>(a.dh, a.lddh, at, v);
-            if (READ_U) load_kept<ANY, V, UT, CKPT>(r.u, g.u, g.ldu, g.u8, g.u8_scales, at, v);
+            r.dh = load_vec<END, V, XT>(a.dh, a.lddh, at, v);
+            if (READ_U) load_kept<END, V, UT, CKPT>(r.u, g.u, g.ldu, g.u8, g.u8_scales, at, v);
         }
     };
     Vec next[MODE == ROW_AHEAD ? V : 1];
@@ -141,12 +143,12 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
         gate_row = begin / g.gate_run;
         in_run = begin - gate_row * g.gate_run;
     }
-    Place at{first, (uint32_t)(begin - first), col0, step, g.cols, g.pitch8, count > 0};
+    Place at{first, (uint32_t)(begin - first), col0, step, g.cols, g.pitch8, count > 0, back_of<END, V>(g.cols, col0, step)};
     fetch(at);
     float* own_gate = lds + vectors * Params::STRIDE + team_in_block * vectors * Params::GATE_STRIDE;     // a lane reads what it wrote
-    auto gate_of_row = [&](int v) { return param8<ANY>(g.gate, g.gate_bf16, gate_row * g.ld_gate + at.col(v), at.left(v), 0.0f); };
+    auto gate_of_row = [&](int v) { return param8<TAIL>(g.gate, g.gate_bf16, gate_row * g.ld_gate + at.col(v), at.left(v), 0.0f); };
     auto take_gate = [&]() {
-        if (PART != BWD_ROWS && g.gate_in_lds) {
+        if (PART != BWD_ROWS) {
 #pragma unroll
             for (int v = 0; v < V; ++v) Params::put(own_gate + (lane + v * g.lanes) * Params::GATE_STRIDE, gate_of_row(v));
         }
@@ -154,13 +156,12 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
     if (gate_by_row) take_gate();
     auto param = [&](NormParam which, int v) {
         if constexpr (PART != BWD_ROWS) {
-            if (which == P_GATE && gate_by_row)
-                return g.gate_in_lds ? Params::get(own_gate + (lane + v * g.lanes) * Params::GATE_STRIDE) : gate_of_row(v);
+            if (which == P_GATE && gate_by_row) return Params::get(own_gate + (lane + v * g.lanes) * Params::GATE_STRIDE);
             return Params::get(lds, Params::STRIDE, which, lane + v * g.lanes);
         } else {
             if (which == P_GATE && gate_by_row) return gate_of_row(v);
             if (g.plane[which] != ParamPlanes::NO_PLANE) return ParamPlanes::get(lds, g.plane[which], vectors, lane + v * g.lanes, param_is_bf16(g, which));
-            return norm_param<ANY>(g, which, col0 + v * step);
+            return norm_param<TAIL>(g, which, col0 + v * step);
         }
     };
     for (uint32_t i = 0; i < (uint32_t)g.team_rows; ++i) {
@@ -178,18 +179,29 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
         ahead.first += g.row_step;
         ahead.live = i + 1 < count;
         fetch(ahead);
-        // one of the lane's vectors at a time; what a step needs of it is loaded again, or taken from its registers
-        auto each = [&](bool h, bool u, auto&& f) {
+        // one of the lane's vectors at a time; what a step needs of it is loaded again, or taken from its registers (first_h,
+        // first_u: for the first time)
+        auto each = [&](bool h, bool u, bool first_h, bool first_u, auto&& f) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 Vec& r = held[MODE == ROW_AGAIN ? 0 : v];
                 if constexpr (MODE == ROW_AGAIN) load(r, at, v, h, u);
+                if (END == ROW_ENDS && v == V - 1) {
+                    if (MODE == ROW_AGAIN ? h : first_h) {
+                        settle(r.dy, at.back);
+                        settle<XT>(r.h, at.back);
+                    }
+                    if (MODE == ROW_AGAIN ? u : first_u) {
+                        settle(r.dh, at.back);
+                        if (READ_U) settle<UT>(r.u, at.back);
+                    }
+                }
                 f(r, v);
                 if (V > 1) __builtin_amdgcn_sched_barrier(0);
             }
         };
         float s[2] = {0.0f, 0.0f};
-        each(true, false, [&](Vec& r, int v) {
+        each(true, false, true, false, [&](Vec& r, int v) {
             const F8 dy = widen(r.dy), h = value_of<XT>(r.h), w = param(P_PRE_WEIGHT, v);
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
@@ -226,13 +238,13 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
         };
         F8 dv[PLAN.keep && POST ? V : 1];
         const float ru = post ? st.y : 1.0f;                             // without a post-norm u itself takes part
-        if constexpr (PART != BWD_SUMS || READ_U) each(true, true, [&](Vec& r, int v) {
+        if constexpr (PART != BWD_SUMS || READ_U) each(true, true, false, true, [&](Vec& r, int v) {
             const F8 dh = gradient(r, v);
             if constexpr (PART != BWD_SUMS) {
                 F8 out;
 #pragma unroll
                 for (int t = 0; t < 8; ++t) out.v[t] = g.rho * dh.v[t];
-                store_vec<ANY, V, XT>(a.dx, a.lddx, at, v, out);
+                store_vec<END, V, XT>(a.dx, a.lddx, at, v, out);
             }
             F8 d, u, w;
 #pragma unroll
@@ -262,7 +274,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
                 }
             }
             if constexpr (!POST) {
-                if constexpr (PART != BWD_SUMS) store_vec<ANY, V, UT>(a.du, a.lddu, at, v, d);
+                if constexpr (PART != BWD_SUMS) store_vec<END, V, UT>(a.du, a.lddu, at, v, d);
             } else {
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
@@ -285,7 +297,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
                 u0 = s[1] * g.inv_cols;
             }
             forget();
-            each(true, true, [&](Vec& r, int v) {
+            each(true, true, false, false, [&](Vec& r, int v) {
                 F8 d;
                 if constexpr (!PLAN.keep) {
                     renew(r.dh);
@@ -307,7 +319,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
                 const F8 u = value_of<UT>(r.u);
 #pragma unroll
                 for (int t = 0; t < 8; ++t) d.v[t] = ru * __builtin_fmaf(-(u.v[t] - st.x) * ru, u1, d.v[t] - u0);
-                store_vec<ANY, V, UT>(a.du, a.lddu, at, v, d);
+                store_vec<END, V, UT>(a.du, a.lddu, at, v, d);
             });
         }
         if (PART != BWD_ROWS && gate_by_row && ++in_run == g.gate_run) {       // the gate's row is complete
@@ -315,8 +327,8 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     const int64_t to = gate_row * g.cols + at.col(v);
-                    if (g.gate_bf16) store8<ANY>(static_cast<uint16_t*>(a.dgate) + to, acc[GATE_SUM][v], at.left(v));
-                    else             store8<ANY>(static_cast<float*>(a.dgate) + to, acc[GATE_SUM][v], at.left(v));
+                    if (g.gate_bf16) store8<TAIL>(static_cast<uint16_t*>(a.dgate) + to, acc[GATE_SUM][v], at.left(v));
+                    else             store8<TAIL>(static_cast<float*>(a.dgate) + to, acc[GATE_SUM][v], at.left(v));
                     acc[GATE_SUM][v] = mxd::zero8();
                 }
             }
@@ -341,7 +353,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
                 if (k < g.teams) {
 #pragma unroll
                     for (int v = 0; v < V; ++v)
-                        store8<ANY>(a.gate_partials + k * g.cols + col0 + v * step, acc[s][v], left(g.cols, col0 + v * step));
+                        store8<TAIL>(a.gate_partials + k * g.cols + col0 + v * step, acc[s][v], left(g.cols, col0 + v * step));
                 }
                 continue;
             }
@@ -349,7 +361,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
         }
         if (teams == 1) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) store8<ANY>(out + col0 + v * step, acc[s][v], left(g.cols, col0 + v * step));
+            for (int v = 0; v < V; ++v) store8<TAIL>(out + col0 + v * step, acc[s][v], left(g.cols, col0 + v * step));
             continue;
         }
         __syncthreads();
@@ -365,15 +377,15 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
 }
 
 template <bool LAYER>
-hipError_t launch_norm_bwd(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, BwdPart part, dim3 grid, uint32_t threads, size_t lds, hipStream_t st)
+hipError_t launch_norm_bwd(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, RowEnd end, int v, BwdPart part, dim3 grid, uint32_t threads, size_t lds, hipStream_t st)
 {
     hipError_t e = hipSuccess;
     by_types(x_bf16, u_bf16, [&](auto xt, auto ut) {
-        by_kind(any, a.f.post, a.f.gate != nullptr, [&](auto post, auto gate, auto odd) {
+        by_kind(end, a.f.post, a.f.gate != nullptr, [&](auto post, auto gate, auto ends) {
             by_flag(eight, [&](auto c) {
                 auto run = [&](auto n, auto which) {
-                    e = start_norm(residual_norm_bwd_kernel<decltype(xt), decltype(ut), decltype(n)::value, decltype(post)::value, decltype(gate)::value,
-                                                            LAYER, decltype(c)::value, decltype(odd)::value, decltype(which)::value>, grid, threads, lds, st, a);
+                    if constexpr (decltype(ends)::value != ROW_SHORT || (decltype(n)::value == 1 && decltype(which)::value == BWD_ALL)) e = start_norm(residual_norm_bwd_kernel<decltype(xt), decltype(ut), decltype(n)::value, decltype(post)::value, decltype(gate)::value,
+                                                            LAYER, decltype(c)::value, decltype(ends)::value, decltype(which)::value>, grid, threads, lds, st, a);
                 };
                 using One = std::integral_constant<int, 1>;
                 if (part == BWD_ROWS)      run(std::integral_constant<int, 4>{}, std::integral_constant<BwdPart, BWD_ROWS>{});

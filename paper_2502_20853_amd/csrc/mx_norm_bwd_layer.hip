@@ -3,9 +3,9 @@
 
 namespace mxl {
 
-hipError_t launch_norm_bwd_layer(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, bool any, int v, BwdPart part, dim3 grid, uint32_t threads, size_t lds, hipStream_t st)
+hipError_t launch_norm_bwd_layer(const NormGradArgs& a, bool x_bf16, bool u_bf16, bool eight, RowEnd end, int v, BwdPart part, dim3 grid, uint32_t threads, size_t lds, hipStream_t st)
 {
-    return launch_norm_bwd<true>(a, x_bf16, u_bf16, eight, any, v, part, grid, threads, lds, st);
+    return launch_norm_bwd<true>(a, x_bf16, u_bf16, eight, end, v, part, grid, threads, lds, st);
 }
 
 }  // namespace mxl

@@ -755,6 +755,67 @@ def test_modules_keep_their_state(mx):
     assert set(mx.MxResidualNorm(64, affine=False, post=True).state_dict()) == set()
 
 
+@pytest.mark.parametrize("d", [40, 41, 1001])
+def test_rows_far_apart(mx, d):
+    """Rows 2^31 bytes apart, as columns of a large matrix: the results are those of dense rows."""
+    g = torch.Generator(device="cuda").manual_seed(21)
+    n, ld = 12, (1 << 30) + 3
+    far = torch.empty(n * ld, device="cuda", dtype=BF).as_strided((n, d), (ld, 1))
+    x, u, p = make(g, n, d, BF, BF, F32, False, True, 3)
+    dh, dy = (torch.randn((n, d), generator=g, device="cuda").to(BF) for _ in range(2))
+
+    def step(x, u, dy):
+        leaves = [t.detach().requires_grad_(True) for t in (x, u, *p.values())]
+        h, y = mx.residual_norm(leaves[0], leaves[1], **dict(zip(p, leaves[2:])), post=True)
+        return (h, y, *torch.autograd.grad((h, y), leaves, (dh, dy)))
+    want = step(x, u, dy)
+    for which in range(3):
+        data = [x, u, dy]
+        far.copy_(data[which])
+        data[which] = far
+        assert data[which].stride(0) == ld
+        # sums over rows go by another split; the rows themselves do not
+        for i, (a, b) in enumerate(zip(step(*data), want)):
+            if i < 4:
+                assert torch.equal(a, b), (which, i)
+            else:
+                torch.testing.assert_close(a, b, rtol=2.0 ** -16, atol=2.0 ** -16 * b.abs().max().item())
+
+
+@pytest.mark.parametrize("off,ld", [(1, 96), (0, 97), (3, 98), (2, 100), (1, 131)])
+@pytest.mark.parametrize("t", [BF, F32])
+def test_rows_at_any_alignment(mx, t, off, ld):
+    """Whole vectors at addresses of no more than their elements' alignment; what lies between the rows stays as it is."""
+    g = torch.Generator(device="cuda").manual_seed(22)
+    n, d = 70, 96
+    x, u, p = make(g, n, d, t, t, F32, True, True, 1)
+    place = lambda: torch.full((n * ld + 8,), 7.0, device="cuda", dtype=t)
+    mem = {k: place() for k in ("x", "u", "dy")}
+    at = {k: m.as_strided((n, d), (ld, 1), off) for k, m in mem.items()}
+    dy = torch.randn((n, d), generator=g, device="cuda").to(t)
+    for k, v in (("x", x), ("u", u), ("dy", dy)):
+        at[k].copy_(v)
+
+    def step(x, u, dy):
+        x, u = x.detach().requires_grad_(True), u.detach().requires_grad_(True)
+        h, y = mx.residual_norm(x, u, **p, norm="layer", post=True)
+        return (h, y, *torch.autograd.grad(y, (x, u), dy))
+    assert all(torch.equal(a, b) for a, b in zip(step(at["x"], at["u"], at["dy"]), step(x, u, dy)))
+    # outputs there, through the C interface
+    import ctypes
+    B = mx.binding
+    out = {k: place() for k in ("h", "y")}
+    want = mx.residual_norm(x, u, post=True)
+    bf = int(t == BF)
+    a = B.ResidualNormArgs(rows=n, cols=d, x=at["x"].data_ptr(), u=at["u"].data_ptr(), ldx=ld, ldu=ld, ldh=ld, ldy=ld, x_dtype=bf, u_dtype=bf, pre=1, post=1,
+                           residual_scale=1.0, branch_scale=1.0, eps=1e-6, **{k: m.data_ptr() + off * t.itemsize for k, m in out.items()})
+    assert B.lib().mx_residual_norm_fwd(ctypes.byref(a), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+    for m, w in zip(out.values(), want):
+        expected = place()
+        expected.as_strided((n, d), (ld, 1), off).copy_(w)
+        assert torch.equal(m, expected)
+
+
 def test_large_offsets(mx):
     """Rows beyond 2^31 elements and 2^32 bytes: the last rows equal those of a small call."""
     n, d = (1 << 31) // 8192 + 40, 8192
