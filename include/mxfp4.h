@@ -499,7 +499,8 @@ int mx_residual_norm_bwd(const mx_residual_norm* p, const mx_residual_norm_grads
  * Activation of an MLP between its two linear layers: a = act(p), p [rows x cols], or gated, p [rows x 2 cols],
  *     a[:, j] = act(p[:, j]) * p[:, cols + j].
  *   MX_ACT_GELU   x Phi(x), Phi the normal distribution function;   MX_ACT_SILU   x / (1 + exp(-x)).
- * FP32; act(x) is within 2^-18 max(|act(x)|, 2^-100) of its exact value for |x| <= 4, and within 2^-15 of that beyond.
+ * FP32; act(x) is within 2^-18 max(|act(x)|, 2^-100) of its exact value for |x| <= 4, and within 2^-15 of that beyond.  A NaN
+ * gives NaN; an infinite x gives act's limit or NaN.
  *   p        device, dtype F32 or BF16, row stride ldp
  *   a        device out, dtype, row stride lda; or NULL with a_codes, a_scales: a as MXFP4 row codes (as y_codes above;
  *            cols % 32 == 0, a_codes 16-byte aligned)

@@ -2,7 +2,10 @@
 // reads the checkpoint in place of p.  And the checkpoint codec by itself.
 //
 // All of them stream: a lane owns eight consecutive elements, four neighbouring lanes a group of 32, and every array is
-// touched once, 16 bytes (8 of codes) a lane.
+// touched once, 16 bytes (8 of codes) a lane.  Bound by memory, GELU by the vector units as well (29 operations an element
+// forward with the checkpoint; busy all of the time, so that its time follows the clock).  bf16 with checkpoints: GELU
+// 50432 x 4096 187 us forward for 1039 MB and 194 backward, gated SiLU 16384 x (2 x 8192) 201 and 202 us for 1082 MB each; a
+// large copy's 5.4 TB/s would take 192 and 200.  Packing 50432 x 1024 in bf16 28 us, unpacking 23.5 (the codes partly cached).
 #include "mx_block.hpp"
 
 #include <algorithm>
@@ -79,7 +82,8 @@ __device__ __forceinline__ float act(float x, float& slope)
 
 constexpr uint32_t THREADS = 256;
 
-// Chunks a lane works on, one workgroup's width apart; their loads go out together.
+// Chunks a lane works on, one workgroup's width apart; their loads go out together.  Gated SiLU backward, 16384 x 16384 bf16: two
+// chunks 201 us, four 202, eight 210; packing 50432 x 1024: 26.6, 26.3, 25.6.
 template <typename T> constexpr int CHUNKS = sizeof(T) == 2 ? 4 : 2;
 
 template <typename T, bool SILU, bool GATED, bool TAIL>
