@@ -413,7 +413,7 @@ int mx_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, int64_t ro
  * FP32 throughout, sums included; the sum of the squares of a row must be finite.
  *   x, u          device, [rows x cols]; x_dtype and u_dtype F32 or BF16, not a BF16 stream with an F32 branch
  *                 (MX_ERR_DTYPE).  u NULL: no block, y = n(x); h, gate, post and the scales are not used then and h must be NULL
- *   h             device out, x_dtype; may be x itself (with ldh = ldx)
+ *   h             device out, x_dtype; may be x itself (with ldh = ldx).  No other output may overlap an input
  *   y             device out, u_dtype; or NULL with
  *   y_codes, y_scales   device out: y as MXFP4 row codes, the Q(1) of mx_quantize with round_D and scale_mode applied to
  *                 the FP32 values, which is what mx_linear_fwd takes as xq, xs.  cols % 32 == 0; y_codes 16-byte aligned

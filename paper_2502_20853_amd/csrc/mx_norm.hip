@@ -142,6 +142,11 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
         }
         settle(u[V - 1], at.back);
         settle(h[V - 1], at.back);
+        if (END == ROW_ENDS && g.in_place) {
+            // the row's last eight elements may be another wave's to overwrite
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+        }
         forget();
         Place next = at;
         next.first += g.row_step;

@@ -48,6 +48,7 @@ struct NormArgs {
     float inv_cols, rho, sigma, eps;
     uint8_t plane[8];                                         // of the parameters in LDS (ParamPlanes)
     bool layer, post, param_bf16, gate_bf16, gate_by_row, floor_mode;
+    bool in_place;                                            // h is x
 };
 
 struct NormGradArgs {
@@ -364,6 +365,7 @@ inline NormArgs norm_args(const ResidualNormParams& p, const TeamShape& shape)
     g.inv_cols = (float)(1.0 / (double)p.cols);
     g.rho = p.residual_scale; g.sigma = p.branch_scale; g.eps = p.eps;
     g.layer = p.layer; g.post = p.post;
+    g.in_place = p.h != nullptr && p.h == p.x;
     g.param_bf16 = p.param_bf16; g.gate_bf16 = p.gate_bf16; g.floor_mode = p.floor_mode;
     return g;
 }

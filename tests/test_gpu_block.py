@@ -816,6 +816,31 @@ def test_rows_at_any_alignment(mx, t, off, ld):
         assert torch.equal(m, expected)
 
 
+@pytest.mark.parametrize("t", [BF, F32])
+@pytest.mark.parametrize("d", [5, 33, 1001, 4099, 9001, 16383])
+@pytest.mark.parametrize("post", [False, True])
+def test_odd_rows_in_place_and_apart(mx, t, d, post):
+    """h over x, and outputs in rows further apart than they are long: only the rows change."""
+    import ctypes
+    B = mx.binding
+    g = torch.Generator(device="cuda").manual_seed(23)
+    n, ld = 600, d + 3
+    x, u, p = make(g, n, d, t, t, F32, False, post, 1)
+    want = mx.residual_norm(x, u, **p, post=post)
+    mem = [torch.full((n * ld,), 7.0, device="cuda", dtype=t) for _ in range(2)]
+    rows = [m.as_strided((n, d), (ld, 1)) for m in mem]
+    rows[0].copy_(x)
+    bf = int(t == BF)
+    a = B.ResidualNormArgs(rows=n, cols=d, x=mem[0].data_ptr(), h=mem[0].data_ptr(), y=mem[1].data_ptr(), u=u.data_ptr(), ldx=ld, ldu=d, ldh=ld, ldy=ld,
+                           x_dtype=bf, u_dtype=bf, pre=1, post=int(post), residual_scale=1.0, branch_scale=1.0, eps=1e-6, gate_rows=1, ld_gate=d,
+                           **{k: v.data_ptr() for k, v in p.items()})
+    assert B.lib().mx_residual_norm_fwd(ctypes.byref(a), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+    for m, w in zip(mem, want):
+        expected = torch.full((n * ld,), 7.0, device="cuda", dtype=t)
+        expected.as_strided((n, d), (ld, 1)).copy_(w)
+        assert torch.equal(m, expected)
+
+
 def test_large_offsets(mx):
     """Rows beyond 2^31 elements and 2^32 bytes: the last rows equal those of a small call."""
     n, d = (1 << 31) // 8192 + 40, 8192
