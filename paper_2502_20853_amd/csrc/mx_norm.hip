@@ -66,8 +66,9 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
 
     // every g.teams-th row, so that the chip works in one window of the matrix at a time; with gate rows a run of rows, so that a
     // team's gate row rarely changes
-    const int64_t k0 = (int64_t)blockIdx.x * teams, k = k0 + team_in_block;
     const bool runs = GATE && g.row_step == 1;
+    const TeamRows own(runs, team_in_block, teams, g.lanes);
+    const int64_t k0 = own.k0, k = own.k;
     const int64_t first = runs ? g.rows * k0 / g.teams : k0, begin = k >= g.teams ? first : runs ? g.rows * k / g.teams : k;
     const uint32_t count = k >= g.teams ? 0u : (uint32_t)(runs ? g.rows * (k + 1) / g.teams - begin : (g.rows - k + g.teams - 1) / g.teams);
     Place at{first, (uint32_t)(begin - first), lane * 8u, step, g.cols, g.pitch8, count > 0, back_of<END, V>(g.cols, lane * 8u, step)};
@@ -322,7 +323,7 @@ hipError_t launch_fwd(const ResidualNormParams& p, hipStream_t st)
         g.teams = std::min<int64_t>(p.rows, (int64_t)grid * teams);
         g.team_rows = (p.rows + g.teams - 1) / g.teams;
         g.row_step = gate_rows ? 1 : g.teams;
-        const int64_t span = (teams + 1) * (gate_rows ? g.team_rows : 1);                // rows that a workgroup's teams reach over
+        const int64_t span = rows_at_once(gate_rows, s.lanes, grid, teams, g.team_rows);
         if (!far && (!covers(p.x, p.x_bf16, p.ldx, span) || !covers(p.u, p.u_bf16, p.ldu, span) || !covers(p.h, p.x_bf16, p.ldh, span) ||
                      !covers(p.y, p.u_bf16, p.ldy, span))) {
             far = true;
@@ -411,7 +412,7 @@ hipError_t launch_residual_norm_bwd(const ResidualNormParams& p, const ResidualN
     const int64_t gate_rows = p.gate != nullptr ? p.gate_rows : 1;
     const bool eight = p.h8 != nullptr || p.u8 != nullptr;
     BwdPlan b = plan_bwd(p.rows, p.cols, gate_rows);
-    const int64_t span = (b.teams_per_block + 1) * (gate_rows > 1 ? b.team_rows : 1);      // rows that a workgroup's teams reach over
+    const int64_t span = rows_at_once(gate_rows > 1, b.shape.lanes, b.grid, b.teams_per_block, b.team_rows);
     if (!covers(d.dh, p.x_bf16, d.lddh, span) || !covers(d.dy, p.u_bf16, d.lddy, span) || !covers(d.dx, p.x_bf16, d.lddx, span) ||
         !covers(d.du, p.u_bf16, d.lddu, span) || (!eight && (!covers(p.h, p.x_bf16, p.ldh, span) || !covers(p.u, p.u_bf16, p.ldu, span))))
         b = plan_bwd(p.rows, p.cols, gate_rows, b.grid);

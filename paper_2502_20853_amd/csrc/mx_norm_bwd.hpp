@@ -64,9 +64,10 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
     constexpr bool READ_U = POST || GATE, TAIL = END != ROW_WHOLE;
     const bool post = POST && (!TAIL || g.post), gate_by_row = GATE && g.gate_by_row;
 
-    const int64_t k0 = (int64_t)blockIdx.x * teams, k = k0 + team_in_block;
     // without gate rows every g.teams-th row, as in the forward pass
     const bool whole = GATE && a.pieces == 0, runs = PART != BWD_ROWS && GATE && g.row_step == 1;
+    const TeamRows own(runs, team_in_block, teams, g.lanes);
+    const int64_t k0 = own.k0, k = own.k;
     auto start_of = [&](int64_t k) {                                     // of a run
         if (whole) return a.gate_rows * k / g.teams * g.gate_run;
         const int64_t group = k / a.pieces, piece = k % a.pieces;
