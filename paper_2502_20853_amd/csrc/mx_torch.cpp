@@ -11,6 +11,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 
+#include <cstring>
+
 #include "../../include/mxfp4.h"
 #include "mx_launch.hpp"
 
@@ -641,12 +643,22 @@ int64_t gate_rows_of(const Tensor& gate, const Tensor& x)
     return rows;
 }
 
-// Everything of a call but its outputs; the tensors it points into live in `keep`.
-mxl::ResidualNormParams norm_params(const NormInputs& in, const NormOptions& o, std::vector<Tensor>& keep, bool copy = true)
+// Everything of a call but its outputs, and the tensors that it points into.
+struct NormCall {
+    mxl::ResidualNormParams p{};
+    std::vector<Tensor> keep;
+    bool stand_in = false;     // x or u has yet to be copied
+};
+
+NormCall norm_call(const NormInputs& in, const NormOptions& o, bool copy)
 {
+    at::AutoDispatchBelowADInplaceOrView guard;               // a view of the gate here is none of the graph's
     const Tensor& x = in.x;
     const int64_t D = x.size(-1);
-    mxl::ResidualNormParams p{};
+    NormCall call;
+    mxl::ResidualNormParams& p = call.p;
+    std::vector<Tensor>& keep = call.keep;
+    keep.reserve(7);
     const Rows xr = rows_of(x, D, copy);
     keep.push_back(xr.t);
     p.x = xr.t.data_ptr(); p.ldx = xr.ld; p.x_bf16 = is_bf16(x);
@@ -683,10 +695,11 @@ mxl::ResidualNormParams norm_params(const NormInputs& in, const NormOptions& o, 
         p.gate = gr.t.data_ptr(); p.ld_gate = gr.ld; p.gate_bf16 = is_bf16(*in.gate);
     }
     p.residual_scale = o.residual_scale; p.branch_scale = o.branch_scale; p.eps = o.eps;
-    return p;
+    call.stand_in = !copy && !((xr.t.is_contiguous() || xr.ld != D) && (!in.u || keep[1].is_contiguous() || p.ldu != D));
+    return call;
 }
 
-void check_norm_call(const NormInputs& in, const NormOptions& o, bool packed)
+NormCall checked_norm_call(const NormInputs& in, const NormOptions& o, bool packed)
 {
     no_trace(NORM);
     const OptTensor x = in.x;
@@ -698,13 +711,13 @@ void check_norm_call(const NormInputs& in, const NormOptions& o, bool packed)
     TORCH_CHECK_VALUE(o.post || (!in.post_weight && !in.post_bias), "post=False takes no post_weight or post_bias");
     TORCH_CHECK_VALUE(o.layer || (!in.pre_bias && !in.post_bias), "an RMS norm has no bias");
     if (in.x.numel() == 0) throw Status("mx_residual_norm_fwd", MX_ERR_SHAPE);
-    std::vector<Tensor> keep;
-    const mxl::ResidualNormParams p = norm_params(in, o, keep, false);
-    check(mxl::check_residual_norm(p), "mx_residual_norm_fwd");
-    if (packed && p.cols % 32 != 0) throw Status("mx_residual_norm_fwd", MX_ERR_SHAPE);
+    NormCall call = norm_call(in, o, false);
+    check(mxl::check_residual_norm(call.p), "mx_residual_norm_fwd");
+    if (packed && call.p.cols % 32 != 0) throw Status("mx_residual_norm_fwd", MX_ERR_SHAPE);
     TORCH_CHECK(in.x.is_cuda(), NORM, " runs on the GPU");
     for (const OptTensor* t : {&in.u, &in.pre_weight, &in.pre_bias, &in.post_weight, &in.post_bias, &in.gate})
         TORCH_CHECK(!*t || (*t)->get_device() == in.x.get_device(), NORM, ": x, u, parameters and gate must be on one GPU");
+    return call;
 }
 
 // What a forward pass leaves for the backward pass.
@@ -726,10 +739,10 @@ struct NormEight {
 };
 
 // Outputs {h or undefined, y or undefined}, packed {h, codes, scales}.
-torch::autograd::variable_list norm_forward(const NormInputs& in, const NormOptions& o, bool packed, bool eight, NormKept* kept)
+torch::autograd::variable_list norm_forward(NormCall& call, const NormInputs& in, const NormOptions& o, bool packed, bool eight, NormKept* kept)
 {
-    std::vector<Tensor> keep;
-    mxl::ResidualNormParams p = norm_params(in, o, keep);
+    if (call.stand_in) call = norm_call(in, o, true);
+    mxl::ResidualNormParams& p = call.p;
     torch::autograd::variable_list out;
     Tensor h, y;
     if (p.branch) {
@@ -764,24 +777,37 @@ torch::autograd::variable_list norm_forward(const NormInputs& in, const NormOpti
     return out;
 }
 
+int64_t bits_of(float v)
+{
+    int32_t b;
+    std::memcpy(&b, &v, sizeof b);
+    return b;
+}
+float float_of(int64_t bits)
+{
+    const int32_t b = (int32_t)bits;
+    float v;
+    std::memcpy(&v, &b, sizeof v);
+    return v;
+}
+
 struct MxResidualNormFn : torch::autograd::Function<MxResidualNormFn> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& x, const OptTensor& u, const OptTensor& pre_weight,
                                                   const OptTensor& pre_bias, const OptTensor& post_weight, const OptTensor& post_bias,
-                                                  const OptTensor& gate, const NormOptions& o, bool eight)
+                                                  const OptTensor& gate, const NormOptions& o, bool eight, NormCall* call)
     {
         at::AutoDispatchBelowADInplaceOrView guard;
         const NormInputs in{x, u, pre_weight, pre_bias, post_weight, post_bias, gate};
         NormKept kept;
-        auto out = norm_forward(in, o, false, eight, &kept);
+        auto out = norm_forward(*call, in, o, false, eight, &kept);
         const bool use_u = u && (o.post || gate);                     // the backward pass looks at u itself
         ctx->set_materialize_grads(false);
         ctx->save_for_backward({kept.stats, kept.eight, eight || !o.pre ? Tensor() : kept.h, eight || !use_u ? Tensor() : *u,
                                 pre_weight.value_or(Tensor()), post_weight.value_or(Tensor()), post_bias.value_or(Tensor()), gate.value_or(Tensor())});
         ctx->saved_data["shape"] = x.sizes().vec();
         auto type = [](const OptTensor& t) { return t ? (int64_t)t->scalar_type() : -1; };
-        ctx->saved_data["types"] = std::vector<int64_t>{(int64_t)x.scalar_type(), type(u), type(pre_weight), type(pre_bias), type(post_weight), type(post_bias), type(gate)};
-        ctx->saved_data["flags"] = std::vector<int64_t>{o.layer, o.pre, o.post, eight};
-        ctx->saved_data["scales"] = std::vector<double>{o.residual_scale, o.branch_scale, o.eps};
+        ctx->saved_data["meta"] = std::vector<int64_t>{(int64_t)x.scalar_type(), type(u), type(pre_weight), type(pre_bias), type(post_weight), type(post_bias), type(gate),
+                                                       o.layer, o.pre, o.post, eight, bits_of(o.residual_scale), bits_of(o.branch_scale), bits_of(o.eps)};
         torch::autograd::variable_list made;
         for (const Tensor& t : out)
             if (t.defined()) made.push_back(t);
@@ -796,10 +822,10 @@ struct MxResidualNormFn : torch::autograd::Function<MxResidualNormFn> {
     static torch::autograd::variable_list backward_pass(torch::autograd::AutogradContext* ctx, const torch::autograd::variable_list& grads)
     {
         const auto keep = ctx->get_saved_variables();
-        const auto shape = ctx->saved_data["shape"].toIntVector(), types = ctx->saved_data["types"].toIntVector(), flags = ctx->saved_data["flags"].toIntVector();
-        const auto scales = ctx->saved_data["scales"].toDoubleVector();
+        const auto shape = ctx->saved_data["shape"].toIntVector(), types = ctx->saved_data["meta"].toIntVector();
+        const int64_t* const flags = &types[7];
         const bool branch = types[1] >= 0, pre = flags[1] != 0, post = flags[2] != 0, eight = flags[3] != 0;
-        torch::autograd::variable_list result(9);
+        torch::autograd::variable_list result(10);
         const Tensor dh_in = branch ? grads[0] : Tensor(), dy_in = pre ? grads[branch ? 1 : 0] : Tensor();
         if (!dh_in.defined() && !dy_in.defined()) return result;
         const Tensor& any = dh_in.defined() ? dh_in : dy_in;
@@ -812,7 +838,7 @@ struct MxResidualNormFn : torch::autograd::Function<MxResidualNormFn> {
         p.layer = flags[0] != 0; p.branch = branch; p.pre = pre; p.post = post;
         p.x_bf16 = (at::ScalarType)types[0] == at::kBFloat16;
         p.u_bf16 = branch ? (at::ScalarType)types[1] == at::kBFloat16 : p.x_bf16;
-        p.residual_scale = (float)scales[0]; p.branch_scale = (float)scales[1]; p.eps = (float)scales[2];
+        p.residual_scale = float_of(flags[4]); p.branch_scale = float_of(flags[5]); p.eps = float_of(flags[6]);
         std::vector<Tensor> hold;                                     // dense copies live until the launch is enqueued
         auto vector_of = [&](const Tensor& t) -> const void* {
             if (!t.defined()) return nullptr;
@@ -920,7 +946,7 @@ std::vector<OptTensor> residual_norm(const Tensor& x, const OptTensor& u, const 
 {
     const NormInputs in{x, u, pre_weight, pre_bias, post_weight, post_bias, gate};
     const NormOptions o{layer, pre, post, floor_of(scale_mode, "mx_residual_norm_fwd"), (float)residual_scale, (float)branch_scale, (float)eps};
-    check_norm_call(in, o, packed);
+    NormCall call = checked_norm_call(in, o, packed);
     c10::hip::HIPGuard device((c10::DeviceIndex)x.get_device());
     const OptTensor xo = x;
     const bool grad = records({&xo, &u, &pre_weight, &pre_bias, &post_weight, &post_bias, &gate});
@@ -929,10 +955,10 @@ std::vector<OptTensor> residual_norm(const Tensor& x, const OptTensor& u, const 
     std::vector<OptTensor> r{u ? OptTensor() : xo};
     torch::autograd::variable_list out;
     if (grad) {
-        out = MxResidualNormFn::apply(x, u, pre_weight, pre_bias, post_weight, post_bias, gate, o, eight);
+        out = MxResidualNormFn::apply(x, u, pre_weight, pre_bias, post_weight, post_bias, gate, o, eight, &call);
     } else {
         at::AutoDispatchBelowADInplaceOrView guard;
-        out = norm_forward(in, o, packed, false, nullptr);
+        out = norm_forward(call, in, o, packed, false, nullptr);
         if (!u) out.erase(out.begin());
     }
     size_t i = 0;
