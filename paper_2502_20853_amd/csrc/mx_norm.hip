@@ -229,13 +229,16 @@ struct NormFinishArgs {
     const float* partials;
     const float* gate_partials;
     void* out[SUMS];
-    uint32_t parts, gate_parts, cols;
+    uint32_t parts, gate_parts, gate_rows, cols;
     bool param_bf16, gate_bf16;
 };
 
 // Adds the workgroups' sums up: 32 columns a workgroup, its 32 parts of 32 lanes each take a run of the partial rows in
 // order (8 of 256, loaded at once), and the runs are added in order.  Eight parts with runs of 32 to 64: 5 to 6.4 us, this: 4 to 4.8.
+// Gate rows of no more than 32 parts: a row to each run.  Backward pass of 16384 x 1024 with 1024 gate rows of two parts: 44.7 us
+// so, 111.6 with a workgroup for each; 256 rows of eight: 43.5 and 58.8.
 constexpr uint32_t FINISH_RUNS = 32;
+__host__ __device__ constexpr bool gate_row_a_run(uint32_t gate_rows, uint32_t gate_parts) { return gate_rows > 1 && gate_parts <= 32; }
 __global__ __launch_bounds__(32 * FINISH_RUNS) void residual_norm_finish_kernel(const NormFinishArgs a)
 {
     __shared__ float part[FINISH_RUNS][33];
@@ -245,6 +248,17 @@ __global__ __launch_bounds__(32 * FINISH_RUNS) void residual_norm_finish_kernel(
     const bool is_gate = y >= SUMS - 1;
     const uint32_t s = is_gate ? GATE_SUM : y >= GATE_SUM ? y + 1 : y;
     if (a.out[s] == nullptr) return;
+    if (is_gate && gate_row_a_run(a.gate_rows, a.gate_parts)) {
+        const uint32_t row = (y - (SUMS - 1)) * FINISH_RUNS + p;
+        if (row >= a.gate_rows || c >= a.cols) return;
+        const float* q = a.gate_partials + (int64_t)row * a.gate_parts * a.cols + c;
+        float t = 0.0f;
+        for (uint32_t b = 0; b < a.gate_parts; ++b) t += q[(int64_t)b * a.cols];
+        const int64_t at = (int64_t)row * a.cols + c;
+        if (a.gate_bf16) static_cast<__bf16*>(a.out[s])[at] = (__bf16)t;
+        else             static_cast<float*>(a.out[s])[at] = t;
+        return;
+    }
     const uint32_t parts = is_gate ? a.gate_parts : a.parts;
     const float* from = is_gate ? a.gate_partials + (int64_t)(y - (SUMS - 1)) * parts * a.cols : a.partials + (int64_t)s * parts * a.cols;
     const uint32_t per = (parts + FINISH_RUNS - 1) / FINISH_RUNS, b0 = min(parts, p * per), b1 = min(parts, b0 + per);
@@ -352,10 +366,18 @@ hipError_t launch_fwd(const ResidualNormParams& p, hipStream_t st)
     return e;
 }
 
+// Whether a backward kernel's parameters and its teams' gate rows fit in LDS.
+bool fit_in_lds(int64_t cols, int64_t gate_rows, bool post, bool gate, bool layer)
+{
+    const TeamShape s = shape_for(cols, 2);
+    return s.v < 4 && param_bytes(s, row_end(cols), post, gate, layer, true, gate_rows > 1 ? whole_waves(NORM_THREADS / s.lanes, s.lanes) : 0) <= NORM_LDS_MAX;
+}
+
 // Shape of a backward launch, the same for every type.  Up to two vectors a lane: with three the sums of all kinds do not fit in
 // registers.  In halves the rows are read twice, which is ahead where one kernel would have to load a row for each of its steps:
 // 2048 x 16384 bf16, RMS norms on both sides, gate, 8-bit checkpoints 277 us in one, 151 in halves; layer norms 467 and 162; the
-// RMS pre-norm alone, of which one kernel would hold the sums, 87 and 104.
+// RMS pre-norm alone, of which one kernel would hold the sums, 87 and 104.  And where the teams' gate rows do not fit in LDS
+// beside the parameters (8192 columns, the larger kinds).
 struct BwdPlan {
     TeamShape shape;
     uint32_t teams_per_block, grid, strips;
@@ -363,14 +385,13 @@ struct BwdPlan {
     bool halves;                             // rows first, then sums (strips of columns, a wave each)
 };
 
+// fits: the parameters fit in LDS (fit_in_lds).
 // far_grid: the workgroups of a launch whose teams are one each (one_team), which takes no more workspace than the other; 0: not so.
-BwdPlan plan_bwd(int64_t rows, int64_t cols, int64_t gate_rows, uint32_t far_grid = 0)
+BwdPlan plan_bwd(int64_t rows, int64_t cols, int64_t gate_rows, bool fits, uint32_t far_grid = 0)
 {
     BwdPlan b{};
     b.shape = shape_for(cols, 2);
-    // also where the parameters of the largest kind and the teams' gate rows do not fit in LDS
-    b.halves = b.shape.v == 4 || (gate_rows > 1 && param_bytes(b.shape, ROW_WHOLE, true, true, true, true,
-                                                               whole_waves(NORM_THREADS / b.shape.lanes, b.shape.lanes)) > NORM_LDS_MAX);
+    b.halves = b.shape.v == 4 || !fits;
     if (b.halves) b.shape = {64, 1};
     b.strips = b.halves ? (uint32_t)((cols + 511) / 512) : 1;
     if (far_grid > 0) b.shape = one_team(b.shape, cols);
@@ -402,20 +423,26 @@ hipError_t launch_residual_norm_fwd(const ResidualNormParams& p, hipStream_t st)
 
 size_t residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_rows)
 {
-    const BwdPlan b = plan_bwd(rows, cols, std::max<int64_t>(1, gate_rows));
-    const int64_t gate = gate_rows > 1 ? (b.pieces > 0 ? b.teams : 0) : b.grid;
-    return (b.halves ? (size_t)rows * sizeof(float2) : 0) + ((size_t)SUMS * b.grid + (size_t)gate) * (size_t)cols * sizeof(float);
+    size_t most = 0;
+    // whether a call goes in halves may depend on its kind: enough for the largest kind and the smallest
+    for (const bool fits : {fit_in_lds(cols, gate_rows, true, true, true), fit_in_lds(cols, gate_rows, false, gate_rows > 0, false)}) {
+        const BwdPlan b = plan_bwd(rows, cols, std::max<int64_t>(1, gate_rows), fits);
+        const int64_t gate = gate_rows > 1 ? (b.pieces > 0 ? b.teams : 0) : b.grid;
+        most = std::max(most, (b.halves ? (size_t)rows * sizeof(float2) : 0) + ((size_t)SUMS * b.grid + (size_t)gate) * (size_t)cols * sizeof(float));
+    }
+    return most;
 }
 
 hipError_t launch_residual_norm_bwd(const ResidualNormParams& p, const ResidualNormGrads& d, hipStream_t st)
 {
     const int64_t gate_rows = p.gate != nullptr ? p.gate_rows : 1;
     const bool eight = p.h8 != nullptr || p.u8 != nullptr;
-    BwdPlan b = plan_bwd(p.rows, p.cols, gate_rows);
+    const bool fits = fit_in_lds(p.cols, gate_rows, p.post, p.gate != nullptr, p.layer);
+    BwdPlan b = plan_bwd(p.rows, p.cols, gate_rows, fits);
     const int64_t span = rows_at_once(gate_rows > 1, b.shape.lanes, b.grid, b.teams_per_block, b.team_rows);
     if (!covers(d.dh, p.x_bf16, d.lddh, span) || !covers(d.dy, p.u_bf16, d.lddy, span) || !covers(d.dx, p.x_bf16, d.lddx, span) ||
         !covers(d.du, p.u_bf16, d.lddu, span) || (!eight && (!covers(p.h, p.x_bf16, p.ldh, span) || !covers(p.u, p.u_bf16, p.ldu, span))))
-        b = plan_bwd(p.rows, p.cols, gate_rows, b.grid);
+        b = plan_bwd(p.rows, p.cols, gate_rows, fits, b.grid);
     const RowEnd end = row_end(p.cols);
     const auto launch = p.layer ? launch_norm_bwd_layer : launch_norm_bwd_rms;
     NormGradArgs a{};
@@ -435,7 +462,8 @@ hipError_t launch_residual_norm_bwd(const ResidualNormParams& p, const ResidualN
     f.out[PRE_WEIGHT] = d.dy ? d.dpre_weight : nullptr; f.out[PRE_BIAS] = d.dy && p.layer ? d.dpre_bias : nullptr;
     f.out[POST_WEIGHT] = p.post ? d.dpost_weight : nullptr; f.out[POST_BIAS] = p.post && p.layer ? d.dpost_bias : nullptr;
     f.out[GATE_SUM] = a.want_gate && b.pieces > 0 ? d.dgate : nullptr;
-    const uint32_t gates = f.out[GATE_SUM] ? (uint32_t)gate_rows : 0;
+    f.gate_rows = (uint32_t)gate_rows;
+    const uint32_t gates = !f.out[GATE_SUM] ? 0 : gate_row_a_run(f.gate_rows, f.gate_parts) ? (f.gate_rows + FINISH_RUNS - 1) / FINISH_RUNS : f.gate_rows;
     bool wanted = gates > 0;
     for (void* o : f.out) wanted = wanted || o != nullptr;
 
