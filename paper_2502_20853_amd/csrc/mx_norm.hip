@@ -185,7 +185,8 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
             if (EIGHT) store_codes8<V>(g.h8, g.h8_scales, at, v, b);
             if (V > 1) __builtin_amdgcn_sched_barrier(0);                // one vector at a time: registers are short
         }
-        const float2 sh = statistics<V, TAIL>(h, team, g, at);
+        float2 sh = make_float2(0.0f, 0.0f);
+        if (g.pre) sh = statistics<V, TAIL>(h, team, g, at);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             renew(h[v]);
@@ -433,10 +434,17 @@ size_t residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_ro
     return most;
 }
 
-hipError_t launch_residual_norm_bwd(const ResidualNormParams& p, const ResidualNormGrads& d, hipStream_t st)
+hipError_t launch_residual_norm_bwd(const ResidualNormParams& given, const ResidualNormGrads& d, hipStream_t st)
 {
-    const int64_t gate_rows = p.gate != nullptr ? p.gate_rows : 1;
+    ResidualNormParams p = given;
     const bool eight = p.h8 != nullptr || p.u8 != nullptr;
+    if (d.dy == nullptr) {
+        // nothing of the pre-norm's term is left: h reads as zero and its weight as one, so that a row of h that is not finite, or
+        // such a weight, does not meet the zeros of dy (the kernel leaves the row's statistics out)
+        p.h = p.h8 = p.h8_scales = nullptr;
+        p.pre_weight = nullptr;
+    }
+    const int64_t gate_rows = p.gate != nullptr ? p.gate_rows : 1;
     const bool fits = fit_in_lds(p.cols, gate_rows, p.post, p.gate != nullptr, p.layer);
     BwdPlan b = plan_bwd(p.rows, p.cols, gate_rows, fits);
     const int64_t span = rows_at_once(gate_rows > 1, b.shape.lanes, b.grid, b.teams_per_block, b.team_rows);

@@ -167,8 +167,10 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
     };
     for (uint32_t i = 0; i < (uint32_t)g.team_rows; ++i) {
         Vec held[MODE == ROW_AGAIN ? 1 : V];
-        const float4 st = sn;
+        float4 st = sn;
         const float2 means = mn;
+        // without dy the gradient of h is dh as it is: zeros for the statistics, which may be no numbers, leave the term of the norm out
+        if (a.dy == nullptr) st.z = st.w = 0.0f;
         if (PART == BWD_ROWS && gate_by_row && at.live) gate_row = at.row() / g.gate_run;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
