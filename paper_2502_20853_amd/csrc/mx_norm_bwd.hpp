@@ -171,6 +171,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
         const float2 means = mn;
         // without dy the gradient of h is dh as it is: zeros for the statistics, which may be no numbers, leave the term of the norm out
         if (a.dy == nullptr) st.z = st.w = 0.0f;
+        if (POST && !post) st.x = 0.0f;
         if (PART == BWD_ROWS && gate_by_row && at.live) gate_row = at.row() / g.gate_run;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -240,7 +241,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
             return dh;
         };
         F8 dv[PLAN.keep && POST ? V : 1];
-        const float ru = post ? st.y : 1.0f;                             // without a post-norm u itself takes part
+        const float ru = post ? st.y : 1.0f;                             // without a post-norm u itself takes part, its mean as 0
         if constexpr (PART != BWD_SUMS || READ_U) each(true, true, false, true, [&](Vec& r, int v) {
             const F8 dh = gradient(r, v);
             if constexpr (PART != BWD_SUMS) {
@@ -321,7 +322,10 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const N
                 renew(r.u);
                 const F8 u = value_of<UT>(r.u);
 #pragma unroll
-                for (int t = 0; t < 8; ++t) d.v[t] = ru * __builtin_fmaf(-(u.v[t] - st.x) * ru, u1, d.v[t] - u0);
+                for (int t = 0; t < 8; ++t) {
+                    const float c = ru * __builtin_fmaf(-(u.v[t] - st.x) * ru, u1, d.v[t] - u0);
+                    d.v[t] = post ? c : d.v[t];                          // u may be infinite
+                }
                 store_vec<END, V, UT>(a.du, a.lddu, at, v, d);
             });
         }
