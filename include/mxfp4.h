@@ -417,7 +417,7 @@ int mx_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, int64_t ro
  *   y             device out, u_dtype; or NULL with
  *   y_codes, y_scales   device out: y as MXFP4 row codes, the Q(1) of mx_quantize with round_D and scale_mode applied to
  *                 the FP32 values, which is what mx_linear_fwd takes as xq, xs.  cols % 32 == 0; y_codes 16-byte aligned
- *   *_weight, *_bias    device, cols values of param_dtype; NULL is 1 and 0
+ *   *_weight, *_bias    device, cols values of param_dtype; NULL is 1 and 0.  Those of a norm that there is not (pre or post 0) are not read
  *   gate          device, gate_dtype, gate_rows rows with stride ld_gate, or NULL; gate_rows divides rows, and each gate
  *                 row is that of rows / gate_rows consecutive rows (1: one for all; the number of sequences; rows)
  *   h8, h8_scales, u8, u8_scales   device out, each pair or NULL: mx_checkpoint_pack of h and of u

@@ -563,7 +563,9 @@ static int residual_norm_params(const mx_residual_norm& a, bool branch, mxl::Res
     p.x_bf16 = a.x_dtype == MX_DTYPE_BF16; p.u_bf16 = a.u_dtype == MX_DTYPE_BF16;
     p.rows = a.rows; p.cols = a.cols;
     p.layer = a.norm == MX_NORM_LAYER; p.branch = branch; p.pre = a.pre == 1; p.post = a.post == 1;
-    p.pre_weight = a.pre_weight; p.pre_bias = a.pre_bias; p.post_weight = a.post_weight; p.post_bias = a.post_bias;
+    // without the norm, and an RMS norm's biases: not read, and not there for the kernels, some of which are compiled for both norms
+    if (p.pre) { p.pre_weight = a.pre_weight; p.pre_bias = p.layer ? a.pre_bias : nullptr; }
+    if (p.post) { p.post_weight = a.post_weight; p.post_bias = p.layer ? a.post_bias : nullptr; }
     p.param_bf16 = a.param_dtype == MX_DTYPE_BF16;
     p.gate = a.gate; p.gate_bf16 = a.gate_dtype == MX_DTYPE_BF16; p.gate_rows = a.gate_rows; p.ld_gate = a.ld_gate;
     p.residual_scale = branch ? a.residual_scale : 1.0f; p.branch_scale = branch ? a.branch_scale : 1.0f; p.eps = a.eps;

@@ -1,5 +1,7 @@
 """Operators between the linear layers on the GPU: values that are not finite, arguments that a norm does not read, results
 that are zero.  Against the definitions in 64 bits (block_ref), with the bounds of test_gpu_block."""
+import ctypes
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -83,3 +85,54 @@ def test_infinite_branch_without_a_post_norm(mx, d, layer, ckpt):
         value, scale, rows = want["gate"]
         clean = lambda t: t.cpu().view(gates, d).masked_fill(touched, 0.0)
         check(clean(dgate), clean(value), clean(scale), BACKWARD_OPS + rows, "d gate")
+
+
+class Call:
+    """A forward and a backward pass through the C interface."""
+
+    def __init__(self, mx, n, d, bf, norm, pre, post, gates, seed=1, **given):
+        self.B, self.n, self.d, self.t = mx.binding, n, d, BF if bf else F32
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rnd = lambda *s: torch.randn(s, generator=g, device="cuda").to(self.t)
+        self.mem = {k: rnd(n, d) for k in ("x", "u", "dh", "dy")}
+        self.mem.update({k: rnd(d) for k in ("pre_weight", "pre_bias", "post_weight", "post_bias")}, gate=rnd(max(gates, 1), d))
+        out = lambda *s, t=self.t: torch.full(s, 4096.0, device="cuda", dtype=t)
+        self.mem.update({k: out(n, d) for k in ("h", "y", "dx", "du")}, stats=out(n, 4, t=F32), dgate=out(max(gates, 1), d))
+        self.mem.update({k: out(d) for k in ("dpre_weight", "dpre_bias", "dpost_weight", "dpost_bias")})
+        need = self.B.lib().mx_residual_norm_workspace_bytes(n, d, gates)
+        self.mem["workspace"] = torch.full((need,), 0x7F, device="cuda", dtype=torch.uint8)      # NaN where it is read unwritten
+        at = lambda *names: {k: self.mem[k].data_ptr() for k in names}
+        self.a = self.B.ResidualNormArgs(rows=n, cols=d, ldx=d, ldu=d, ldh=d, ldy=d, x_dtype=int(bf), u_dtype=int(bf), norm=norm, pre=pre, post=post,
+                                         param_dtype=int(bf), gate_dtype=int(bf), gate_rows=gates, ld_gate=d, residual_scale=1.25, branch_scale=0.7,
+                                         eps=1e-6, **at("x", "u", "h", "stats", *(["y"] if pre else []), *(["gate"] if gates else [])))
+        self.b = self.B.ResidualNormGrads(branch=1, lddh=d, lddy=d, lddx=d, lddu=d, workspace_bytes=need, **at("dh", "dx", "du", "workspace"))
+        self.at = at
+
+    def run(self, a=(), b=()):
+        """Both passes with these arguments given as well; what came out of them."""
+        for names, to in ((a, self.a), (b, self.b)):
+            for k, v in self.at(*names).items():
+                setattr(to, k, v)
+        st = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        assert self.B.lib().mx_residual_norm_fwd(ctypes.byref(self.a), st) == 0
+        assert self.B.lib().mx_residual_norm_bwd(ctypes.byref(self.a), ctypes.byref(self.b), st) == 0
+        return {k: self.mem[k].clone() for k in ("h", "y", "dx", "du", "dgate", "dpre_weight", "dpre_bias", "dpost_weight", "dpost_bias", "stats")}
+
+
+@pytest.mark.parametrize("d", [5, 40, 41, 1001, 1024, 8200, 8203])
+@pytest.mark.parametrize("norm", [0, 1])
+def test_weights_of_a_norm_that_there_is_not(mx, d, norm):
+    """Weights and biases that stand in the arguments without their norm, and an RMS norm's biases, change nothing."""
+    for i, (pre, post) in enumerate(((1, 0), (0, 1), (0, 0), (1, 1))):
+        for gates in (0, 1, 3):
+            print("norms", pre, post, gates, flush=True)
+            call = lambda: Call(mx, 6, d, bool(i % 2), norm, pre, post, gates, seed=i)
+            wanted = (["dgate"] if gates else []) + (["dy", "dpre_weight"] if pre else []) + (["dpost_weight"] if post else [])
+            own = (["pre_weight"] if pre else []) + (["post_weight"] if post else [])
+            if norm == 1:
+                own += (["pre_bias"] if pre else []) + (["post_bias"] if post else [])
+            want = call().run(own, wanted)
+            got = call().run(("pre_weight", "pre_bias", "post_weight", "post_bias"), wanted)
+            for k in want:
+                if k != "stats":
+                    assert torch.equal(got[k], want[k]), (pre, post, gates, k)
