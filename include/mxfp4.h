@@ -470,7 +470,8 @@ int mx_residual_norm_fwd(const mx_residual_norm* p, void* stream);
  *         NULL.  branch tells whether there was a block.
  *   dh, dy      device, x_dtype and u_dtype; one of them may be NULL and is zero then; dy needs pre
  *   dx, du      device out, x_dtype and u_dtype, each or NULL
- *   dpre_weight, dpre_bias, dpost_weight, dpost_bias   device out, cols values of param_dtype, each or NULL
+ *   dpre_weight, dpre_bias, dpost_weight, dpost_bias   device out, cols values of param_dtype, each or NULL; zeros without dy (pre),
+ *               for a norm that there is not, and for an RMS norm's bias
  *   dgate       device out, [gate_rows x cols] dense, gate_dtype, or NULL
  *   workspace   device, 16-byte aligned, mx_residual_norm_workspace_bytes(rows, cols, gate_rows) bytes (gate_rows 0
  *               without a gate; 0 for sizes that no call takes); MX_ERR_WORKSPACE if NULL or smaller.  Not kept between

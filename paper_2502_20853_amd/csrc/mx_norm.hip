@@ -231,6 +231,7 @@ struct NormFinishArgs {
     const float* gate_partials;
     void* out[SUMS];
     uint32_t parts, gate_parts, gate_rows, cols;
+    uint32_t none;             // bit s: the call has no part of sum s, which is zero
     bool param_bf16, gate_bf16;
 };
 
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(32 * FINISH_RUNS) void residual_norm_finish_kernel(
         else             static_cast<float*>(a.out[s])[at] = t;
         return;
     }
-    const uint32_t parts = is_gate ? a.gate_parts : a.parts;
+    const uint32_t parts = is_gate ? a.gate_parts : (a.none >> s & 1u) ? 0u : a.parts;
     const float* from = is_gate ? a.gate_partials + (int64_t)(y - (SUMS - 1)) * parts * a.cols : a.partials + (int64_t)s * parts * a.cols;
     const uint32_t per = (parts + FINISH_RUNS - 1) / FINISH_RUNS, b0 = min(parts, p * per), b1 = min(parts, b0 + per);
     float t = 0.0f;
@@ -467,8 +468,9 @@ hipError_t launch_residual_norm_bwd(const ResidualNormParams& given, const Resid
     f.partials = a.partials; f.gate_partials = a.gate_partials;
     f.parts = b.grid; f.gate_parts = gate_rows > 1 ? (uint32_t)b.pieces : b.grid; f.cols = (uint32_t)p.cols;
     f.param_bf16 = p.param_bf16; f.gate_bf16 = p.gate_bf16;
-    f.out[PRE_WEIGHT] = d.dy ? d.dpre_weight : nullptr; f.out[PRE_BIAS] = d.dy && p.layer ? d.dpre_bias : nullptr;
-    f.out[POST_WEIGHT] = p.post ? d.dpost_weight : nullptr; f.out[POST_BIAS] = p.post && p.layer ? d.dpost_bias : nullptr;
+    f.out[PRE_WEIGHT] = d.dpre_weight; f.out[PRE_BIAS] = d.dpre_bias; f.out[POST_WEIGHT] = d.dpost_weight; f.out[POST_BIAS] = d.dpost_bias;
+    const bool part[] = {d.dy != nullptr, p.post, true, d.dy != nullptr && p.layer, p.post && p.layer};       // as NormSum
+    for (int s = 0; s < SUMS; ++s) f.none |= part[s] ? 0u : 1u << s;
     f.out[GATE_SUM] = a.want_gate && b.pieces > 0 ? d.dgate : nullptr;
     f.gate_rows = (uint32_t)gate_rows;
     const uint32_t gates = !f.out[GATE_SUM] ? 0 : gate_row_a_run(f.gate_rows, f.gate_parts) ? (f.gate_rows + FINISH_RUNS - 1) / FINISH_RUNS : f.gate_rows;

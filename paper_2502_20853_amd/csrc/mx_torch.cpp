@@ -902,8 +902,10 @@ struct MxResidualNormFn : torch::autograd::Function<MxResidualNormFn> {
         d.dpre_weight = wanted(2, {D}); d.dpre_bias = wanted(3, {D});
         d.dpost_weight = wanted(4, {D}); d.dpost_bias = wanted(5, {D});
         d.dgate = wanted(6, keep[7].defined() ? keep[7].sizes() : at::IntArrayRef());
-        if (!dy_in.defined())                                         // nothing of y was used
+        if (!dy_in.defined()) {                                       // nothing of y was used
+            d.dpre_weight = d.dpre_bias = nullptr;
             for (int i : {2, 3}) result[i] = Tensor();
+        }
         const size_t bytes = mxl::residual_norm_workspace_bytes(p.rows, D, p.gate ? p.gate_rows : 0);
         const Tensor workspace = at::empty({(int64_t)bytes}, like.dtype(at::kByte));
         d.workspace = workspace.data_ptr();

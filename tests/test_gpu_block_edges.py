@@ -136,3 +136,21 @@ def test_weights_of_a_norm_that_there_is_not(mx, d, norm):
             for k in want:
                 if k != "stats":
                     assert torch.equal(got[k], want[k]), (pre, post, gates, k)
+
+
+@pytest.mark.parametrize("d", [5, 40, 41, 1001, 1024, 8200, 8203])
+@pytest.mark.parametrize("norm", [0, 1])
+@pytest.mark.parametrize("bf", [False, True])
+def test_gradients_of_what_has_no_part_are_zero(mx, d, norm, bf):
+    """Every gradient that is asked for is written: zeros where dy is NULL and where there is no such norm or bias."""
+    params = ("pre_weight", "pre_bias", "post_weight", "post_bias")
+    for pre, post, dy in ((1, 1, 0), (1, 1, 1), (1, 0, 1), (1, 0, 0), (0, 1, 0), (0, 0, 0)):
+        for gates in (0, 1, 3):
+            print("zeros", pre, post, dy, gates, flush=True)
+            got = Call(mx, 6, d, bf, norm, pre, post, gates).run(params, ["d" + k for k in params] + (["dy"] if dy else []) + (["dgate"] if gates else []))
+            for k, part in (("pre_weight", pre and dy), ("pre_bias", pre and dy and norm), ("post_weight", post), ("post_bias", post and norm)):
+                r = got["d" + k]
+                assert torch.isfinite(r).all() and not (r == 4096.0).any(), k
+                assert part or not r.any(), (k, pre, post, dy, gates)
+                assert not part or r.any(), (k, pre, post, dy, gates)
+            assert not gates or (torch.isfinite(got["dgate"]).all() and not (got["dgate"] == 4096.0).any())
