@@ -806,8 +806,10 @@ struct MxResidualNormFn : torch::autograd::Function<MxResidualNormFn> {
                                 pre_weight.value_or(Tensor()), post_weight.value_or(Tensor()), post_bias.value_or(Tensor()), gate.value_or(Tensor())});
         ctx->saved_data["shape"] = x.sizes().vec();
         auto type = [](const OptTensor& t) { return t ? (int64_t)t->scalar_type() : -1; };
-        ctx->saved_data["meta"] = std::vector<int64_t>{(int64_t)x.scalar_type(), type(u), type(pre_weight), type(pre_bias), type(post_weight), type(post_bias), type(gate),
-                                                       o.layer, o.pre, o.post, eight, bits_of(o.residual_scale), bits_of(o.branch_scale), bits_of(o.eps)};
+        std::vector<int64_t> meta{(int64_t)x.scalar_type(), type(u), type(pre_weight), type(pre_bias), type(post_weight), type(post_bias), type(gate),
+                                  o.layer, o.pre, o.post, eight, bits_of(o.residual_scale), bits_of(o.branch_scale), bits_of(o.eps)};
+        if (gate) meta.insert(meta.end(), gate->sizes().begin(), gate->sizes().end());
+        ctx->saved_data["meta"] = std::move(meta);
         torch::autograd::variable_list made;
         for (const Tensor& t : out)
             if (t.defined()) made.push_back(t);
@@ -839,24 +841,30 @@ struct MxResidualNormFn : torch::autograd::Function<MxResidualNormFn> {
         p.x_bf16 = (at::ScalarType)types[0] == at::kBFloat16;
         p.u_bf16 = branch ? (at::ScalarType)types[1] == at::kBFloat16 : p.x_bf16;
         p.residual_scale = float_of(flags[4]); p.branch_scale = float_of(flags[5]); p.eps = float_of(flags[6]);
+        // what the forward pass saved may have gone through a program's pack and unpack hooks
+        auto there = [&](const Tensor& t) { return t.get_device() == any.get_device(); };
         std::vector<Tensor> hold;                                     // dense copies live until the launch is enqueued
-        auto vector_of = [&](const Tensor& t) -> const void* {
-            if (!t.defined()) return nullptr;
-            hold.push_back(t.contiguous());
+        auto saved = [&](int k, int input, at::IntArrayRef sizes) -> const Tensor& {
+            const Tensor& t = keep[k];
+            if (!t.defined() || t.sizes() != sizes || (int64_t)t.scalar_type() != types[input] || !there(t)) throw Status("mx_residual_norm_bwd", MX_ERR_SHAPE);
+            return t;
+        };
+        auto vector_of = [&](int k, int input) -> const void* {
+            if (types[input] < 0) return nullptr;
+            hold.push_back(saved(k, input, D).contiguous());
             return hold.back().data_ptr();
         };
-        p.pre_weight = vector_of(keep[4]); p.post_weight = vector_of(keep[5]); p.post_bias = vector_of(keep[6]);
+        p.pre_weight = vector_of(4, 2); p.post_weight = vector_of(5, 4); p.post_bias = vector_of(6, 5);
         for (int i = 2; i < 6; ++i)
             if (types[i] >= 0) p.param_bf16 = (at::ScalarType)types[i] == at::kBFloat16;
-        if (keep[7].defined()) {
-            const Tensor& gate = keep[7];
+        const at::IntArrayRef gate_sizes(types.data() + 14, types.size() - 14);
+        if (types[6] >= 0) {
+            const Tensor& gate = saved(7, 6, gate_sizes);
             p.gate_rows = gate.numel() / D;
             const Rows gr = rows_of(gate.dim() == 2 ? gate : gate.reshape({p.gate_rows, D}), D);
             hold.push_back(gr.t);
             p.gate = gr.t.data_ptr(); p.ld_gate = gr.ld; p.gate_bf16 = is_bf16(gate);
         }
-        // what the forward pass saved may have gone through a program's pack and unpack hooks
-        auto there = [&](const Tensor& t) { return t.get_device() == any.get_device(); };
         if (stats.scalar_type() != at::kFloat || stats.numel() != 4 * p.rows || !stats.is_contiguous() || !there(stats)) throw Status("mx_residual_norm_bwd", MX_ERR_SHAPE);
         p.stats = const_cast<float*>(stats.data_ptr<float>());
         const bool use_u = branch && (post || p.gate);
@@ -869,7 +877,7 @@ struct MxResidualNormFn : torch::autograd::Function<MxResidualNormFn> {
             if (use_u) { p.u8 = b + e.u.codes; p.u8_scales = b + e.u.scales; }
         } else {
             auto matrix = [&](const Tensor& t, bool bf16, int64_t& ld) -> void* {
-                if (t.numel() != p.rows * D || is_bf16(t) != bf16 || !there(t)) throw Status("mx_residual_norm_bwd", MX_ERR_SHAPE);
+                if (t.sizes() != at::IntArrayRef(shape) || is_bf16(t) != bf16 || !there(t)) throw Status("mx_residual_norm_bwd", MX_ERR_SHAPE);
                 const Rows r = rows_of(t, D);
                 hold.push_back(r.t);
                 ld = r.ld;
@@ -901,7 +909,7 @@ struct MxResidualNormFn : torch::autograd::Function<MxResidualNormFn> {
         d.du = wanted(1, shape); d.lddu = D;
         d.dpre_weight = wanted(2, {D}); d.dpre_bias = wanted(3, {D});
         d.dpost_weight = wanted(4, {D}); d.dpost_bias = wanted(5, {D});
-        d.dgate = wanted(6, keep[7].defined() ? keep[7].sizes() : at::IntArrayRef());
+        d.dgate = wanted(6, gate_sizes);
         if (!dy_in.defined()) {                                       // nothing of y was used
             d.dpre_weight = d.dpre_bias = nullptr;
             for (int i : {2, 3}) result[i] = Tensor();

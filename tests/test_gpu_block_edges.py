@@ -154,3 +154,41 @@ def test_gradients_of_what_has_no_part_are_zero(mx, d, norm, bf):
                 assert part or not r.any(), (k, pre, post, dy, gates)
                 assert not part or r.any(), (k, pre, post, dy, gates)
             assert not gates or (torch.isfinite(got["dgate"]).all() and not (got["dgate"] == 4096.0).any())
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+def test_saved_tensors_that_come_back_as_others(mx, ckpt):
+    """A parameter, gate or matrix that saved-tensor hooks hand back with another type, size, shape or place is refused; one
+    with other strides, or a copy, is taken."""
+    n, d = 96, 64
+    g = torch.Generator(device="cuda").manual_seed(31)
+    x, u, p = make(g, n, d, BF, BF, BF, True, True, 3)
+    leaves = {"x": x, "u": u, **p}
+    for t in leaves.values():
+        t.requires_grad_(True)
+    dh, dy = (torch.randn((n, d), generator=g, device="cuda").to(BF) for _ in range(2))
+
+    def step(name=None, change=None):
+        mine = leaves[name].data_ptr() if name in leaves else None
+
+        def pack(t):
+            hit = t.data_ptr() == mine if mine else name == "h" and t.shape == x.shape and t.data_ptr() != u.data_ptr()
+            seen.append(hit)
+            return hit, t
+        seen = []
+        with torch.autograd.graph.saved_tensors_hooks(pack, lambda s: change(s[1]) if s[0] else s[1]):
+            out = mx.residual_norm(x, u, **p, norm="layer", post=True, checkpoint=ckpt)
+        assert name is None or sum(seen) == 1, name
+        return torch.autograd.grad(out, list(leaves.values()), (dh, dy))
+    want = step()
+    spread = lambda t: torch.stack([t, t], -1).flatten(-2)[..., ::2]
+    for name in ("pre_weight", "post_weight", "post_bias", "gate") + (() if ckpt else ("h", "u")):
+        for same in (torch.clone, spread):
+            assert all(torch.equal(a, b) for a, b in zip(step(name, same), want)), name
+        other = [lambda t: t.float(), lambda t: t.half(), lambda t: t[..., :-1], lambda t: t.cpu(), lambda t: t.unsqueeze(0), lambda t: t.reshape(-1)[:1]]
+        if name in ("gate", "h", "u"):
+            other += [lambda t: t.t().contiguous(), lambda t: t[:1], lambda t: t.reshape(-1)]
+        for i, change in enumerate(other):
+            print("hook", name, i, flush=True)
+            with pytest.raises((mx.MxError, TypeError)):
+                step(name, change)
