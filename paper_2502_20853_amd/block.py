@@ -64,9 +64,11 @@ class MxResidualNorm(torch.nn.Module):
         self.gate = vector(gate is not None, 0 if gate is None else gate)
 
     def forward(self, x, u=None, gate=None, packed=False):
-        """(h, y); without u the norm of x alone (the first block's input)."""
+        """(h, y); without u the pre-norm of x alone (the first block's input), which a module with pre=False has not."""
         if gate is not None and self.gate is not None:
             raise ValueError("this module has a gate of its own")
+        if u is None and (gate is not None or not self.pre):
+            raise ValueError("without a branch u there is only the pre-norm of x: no gate, and a module with pre=True")
         pre = dict(pre_weight=self.pre_weight, pre_bias=self.pre_bias, norm=self.norm, eps=self.eps, checkpoint=self.checkpoint, packed=packed)
         if u is None:
             return residual_norm(x, **pre)

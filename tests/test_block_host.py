@@ -254,3 +254,19 @@ def test_checkpoint_of_scattered_values_on_a_given_stream(mx):
     for values in (torch.zeros(4, 64), torch.zeros(4, 128)[:, :64], torch.zeros(2, 4, 64)):
         with pytest.raises(RuntimeError, match="GPU"):
             mx.mx_checkpoint_pack(values, stream=1)
+
+
+def test_module_without_a_branch_refuses_what_needs_one(mx):
+    """A gate, or a module without a pre-norm, has no part in the norm of x alone."""
+    x, w = torch.zeros(6, 64), torch.ones(64)
+    for kw in (dict(), dict(norm="layer"), dict(post=True), dict(gate=0.5)):
+        with pytest.raises(ValueError):
+            mx.MxResidualNorm(64, device="cpu", **kw)(x, gate=w)
+        with pytest.raises(ValueError):
+            mx.MxResidualNorm(64, device="cpu", pre=False, **kw)(x)
+        with pytest.raises(ValueError):
+            mx.MxResidualNorm(64, device="cpu", pre=False, **kw)(x, packed=True)
+        with pytest.raises(RuntimeError, match="GPU"):                    # these are calls
+            mx.MxResidualNorm(64, device="cpu", **kw)(x)
+        with pytest.raises(RuntimeError, match="GPU"):
+            mx.MxResidualNorm(64, device="cpu", pre=False, **kw)(x, x)
