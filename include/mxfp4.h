@@ -412,9 +412,10 @@ int mx_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, int64_t ro
  *   MX_NORM_LAYER  n(a; w, b) = (a - mean(a)) r w + b,   r = 1 / sqrt(var(a) + eps)
  * FP32 throughout, sums included; the sum of the squares of a row must be finite.
  *   x, u          device, [rows x cols]; x_dtype and u_dtype F32 or BF16, not a BF16 stream with an F32 branch
- *                 (MX_ERR_DTYPE).  u NULL: no block, y = n(x); h, gate, post and the scales are not used then and h must be NULL
- *   h             device out, x_dtype; may be x itself (with ldh = ldx).  No other output may overlap an input
- *   y             device out, u_dtype; or NULL with
+ *                 (MX_ERR_DTYPE).  u NULL: no block, y = n(x); h and gate must be NULL then, pre 1 and post 0, and the scales
+ *                 are not used
+ *   h             device out, x_dtype, required with u; may be x itself (with ldh = ldx).  No other output may overlap an input
+ *   y             device out, u_dtype, required with pre; or NULL with
  *   y_codes, y_scales   device out: y as MXFP4 row codes, the Q(1) of mx_quantize with round_D and scale_mode applied to
  *                 the FP32 values, which is what mx_linear_fwd takes as xq, xs.  cols % 32 == 0; y_codes 16-byte aligned
  *   *_weight, *_bias    device, cols values of param_dtype; NULL is 1 and 0.  Those of a norm that there is not (pre or post 0) are not read
@@ -424,7 +425,7 @@ int mx_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, int64_t ro
  *   stats         device out, FP32 [rows][4], 16-byte aligned, or NULL: mean and r of u, mean and r of h, for the backward
  *                 pass (the mean 0 for MX_NORM_RMS; unspecified where there is no such norm)
  * 1 <= cols <= 16384, rows * cols <= 2^35 - 2^19 (cols rounded up to whole groups); eps at least 2^-126 (MX_ERR_MODE); pointers at the alignment of their elements
- * unless stated.  At least one of h and y is asked for.
+ * unless stated.
  */
 enum { MX_NORM_RMS = 0, MX_NORM_LAYER = 1 };
 typedef struct mx_residual_norm {
@@ -469,7 +470,7 @@ int mx_residual_norm_fwd(const mx_residual_norm* p, void* stream);
  *         either is set.  h (x, where there is no block) is read if dy is given, u with post or dgate; else they may be
  *         NULL.  branch tells whether there was a block.
  *   dh, dy      device, x_dtype and u_dtype; one of them may be NULL and is zero then; dy needs pre
- *   dx, du      device out, x_dtype and u_dtype, each or NULL
+ *   dx, du      device out, x_dtype and u_dtype, each or NULL.  No output may overlap an input
  *   dpre_weight, dpre_bias, dpost_weight, dpost_bias   device out, cols values of param_dtype, each or NULL; zeros without dy (pre),
  *               for a norm that there is not, and for an RMS norm's bias
  *   dgate       device out, [gate_rows x cols] dense, gate_dtype, or NULL

@@ -48,8 +48,8 @@ constexpr RowPlan row_plan()
 // run is one of `pieces` parts of one gate row, or it is a number of whole ones and the team writes them out itself.
 //
 // Up to nine FP32 vectors of the row's length would live in registers: the sums do, the parameters are read from LDS
-// (with four vectors a lane from cache), and what a row needs again behind its sums is kept as loaded.  What is missing (a
-// gradient, a weight) reads as zero or one, so that the loop has next to no branches.
+// (with four vectors a lane from ParamPlanes, and from cache what has no plane there), and what a row needs again behind its
+// sums is kept as loaded.  What is missing (a gradient, a weight) reads as zero or one, so that the loop has next to no branches.
 template <typename XT, typename UT, int V, bool POST, bool GATE, bool LAYER, bool CKPT, RowEnd END, BwdPart PART>
 __global__ __launch_bounds__(NORM_THREADS) void residual_norm_bwd_kernel(const NormGradArgs a)
 {
