@@ -423,7 +423,7 @@ int mx_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, int64_t ro
  *                 row is that of rows / gate_rows consecutive rows (1: one for all; the number of sequences; rows)
  *   h8, h8_scales, u8, u8_scales   device out, each pair or NULL: mx_checkpoint_pack of h and of u
  *   stats         device out, FP32 [rows][4], 16-byte aligned, or NULL: mean and r of u, mean and r of h, for the backward
- *                 pass (the mean 0 for MX_NORM_RMS; unspecified where there is no such norm)
+ *                 pass (the mean 0 for MX_NORM_RMS; those of u 0 without post, those of h unspecified without pre)
  * 1 <= cols <= 16384, rows * cols <= 2^35 - 2^19 (cols rounded up to whole groups); eps at least 2^-126 (MX_ERR_MODE); pointers at the alignment of their elements
  * unless stated.
  */

@@ -185,8 +185,7 @@ __global__ __launch_bounds__(NORM_THREADS) void residual_norm_fwd_kernel(const N
             if (EIGHT) store_codes8<V>(g.h8, g.h8_scales, at, v, b);
             if (V > 1) __builtin_amdgcn_sched_barrier(0);                // one vector at a time: registers are short
         }
-        float2 sh = make_float2(0.0f, 0.0f);
-        if (g.pre) sh = statistics<V, TAIL>(h, team, g, at);
+        const float2 sh = statistics<V, TAIL>(h, team, g, at);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             renew(h[v]);
@@ -441,9 +440,10 @@ hipError_t launch_residual_norm_bwd(const ResidualNormParams& given, const Resid
     const bool eight = p.h8 != nullptr || p.u8 != nullptr;
     if (d.dy == nullptr) {
         // nothing of the pre-norm's term is left: h reads as zero and its weight as one, so that a row of h that is not finite, or
-        // such a weight, does not meet the zeros of dy (the kernel leaves the row's statistics out)
+        // such a weight, does not meet the zeros of dy; nor does a row's statistics (zeros, where the kernel does not leave them out)
         p.h = p.h8 = p.h8_scales = nullptr;
         p.pre_weight = nullptr;
+        if (!p.post) p.stats = nullptr;
     }
     const int64_t gate_rows = p.gate != nullptr ? p.gate_rows : 1;
     const bool fits = fit_in_lds(p.cols, gate_rows, p.post, p.gate != nullptr, p.layer);

@@ -47,7 +47,7 @@ struct NormArgs {
     uint32_t cols, pitch8, lanes;
     float inv_cols, rho, sigma, eps;
     uint8_t plane[8];                                         // of the parameters in LDS (ParamPlanes)
-    bool layer, pre, post, param_bf16, gate_bf16, gate_by_row, floor_mode;
+    bool layer, post, param_bf16, gate_bf16, gate_by_row, floor_mode;
     bool in_place;                                            // h is x
 };
 
@@ -380,7 +380,7 @@ inline NormArgs norm_args(const ResidualNormParams& p, const TeamShape& shape)
     g.lanes = shape.lanes;
     g.inv_cols = (float)(1.0 / (double)p.cols);
     g.rho = p.residual_scale; g.sigma = p.branch_scale; g.eps = p.eps;
-    g.layer = p.layer; g.pre = p.pre; g.post = p.post;
+    g.layer = p.layer; g.post = p.post;
     g.in_place = p.h != nullptr && p.h == p.x;
     g.param_bf16 = p.param_bf16; g.gate_bf16 = p.gate_bf16; g.floor_mode = p.floor_mode;
     return g;
