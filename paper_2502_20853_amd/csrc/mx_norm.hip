@@ -288,7 +288,8 @@ __global__ __launch_bounds__(32 * FINISH_RUNS) void residual_norm_finish_kernel(
     }
 }
 
-// Rows whose parameters do not fit in LDS one by one (ParamPlanes).
+// Rows whose parameters do not fit in LDS one by one (ParamPlanes).  The forward kernel holds the next row beside this one, which with
+// four vectors is more than a lane's registers: 20 to 356 bytes of scratch a lane in whole rows with a post-norm, about 1000 in odd ones.
 TeamShape four_vectors(int64_t cols) { return {lanes_for((cols + 31) / 32), 4}; }
 
 // The shape that wastes the fewest lanes, of those that keep a row in one wave if there is one.  50432 x 768 bf16, layer norms on

@@ -27,6 +27,8 @@ enum RowMode { ROW_AGAIN, ROW_HELD, ROW_AHEAD };
 
 // By the registers that the sums, the raw row (twice) and the gradient that is passed on take, of the 256 a lane has.
 // keep: also whether that gradient is kept between the second step and the third, or computed again.
+// With four vectors a lane (BWD_ROWS) more registers are taken than counted here: 44 to 272 bytes of scratch a lane in whole rows
+// with a post-norm, up to 892 in odd ones.
 struct RowPlan {
     RowMode mode;
     bool keep;
