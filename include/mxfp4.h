@@ -469,7 +469,8 @@ int mx_residual_norm_fwd(const mx_residual_norm* p, void* stream);
  *         gate and scales, stats, and h and u as the forward pass left them, or h8 and u8 (with scales) in their place if
  *         either is set.  h (x, where there is no block) is read if dy is given, u with post or dgate; else they may be
  *         NULL.  branch tells whether there was a block.
- *   dh, dy      device, x_dtype and u_dtype; one of them may be NULL and is zero then; dy needs pre
+ *   dh, dy      device, x_dtype and u_dtype; one of them may be NULL and is zero then; dy needs pre.  Without dy t is dh,
+ *               whatever h holds
  *   dx, du      device out, x_dtype and u_dtype, each or NULL.  No output may overlap an input
  *   dpre_weight, dpre_bias, dpost_weight, dpost_bias   device out, cols values of param_dtype, each or NULL; zeros without dy (pre),
  *               for a norm that there is not, and for an RMS norm's bias

@@ -441,7 +441,8 @@ hipError_t launch_residual_norm_bwd(const ResidualNormParams& given, const Resid
     const bool eight = p.h8 != nullptr || p.u8 != nullptr;
     if (d.dy == nullptr) {
         // nothing of the pre-norm's term is left: h reads as zero and its weight as one, so that a row of h that is not finite, or
-        // such a weight, does not meet the zeros of dy; nor does a row's statistics (zeros, where the kernel does not leave them out)
+        // such a weight, does not meet the zeros of dy; nor do the statistics, which a kernel with a post-norm masks, and another
+        // does without
         p.h = p.h8 = p.h8_scales = nullptr;
         p.pre_weight = nullptr;
         if (!p.post) p.stats = nullptr;

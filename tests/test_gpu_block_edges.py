@@ -192,3 +192,34 @@ def test_saved_tensors_that_come_back_as_others(mx, ckpt):
             print("hook", name, i, flush=True)
             with pytest.raises((mx.MxError, TypeError)):
                 step(name, change)
+
+
+@pytest.mark.parametrize("d", [40, 41, 8200])
+@pytest.mark.parametrize("norm", [0, 1])
+def test_norm_alone_through_the_c_interface(mx, d, norm):
+    """Without a block the post-norm's gradients are zeros too, and the others those of the norm."""
+    n = 6
+    call = Call(mx, n, d, False, norm, 1, 0, 0)
+    call.a.u = call.a.h = call.b.dh = call.b.du = None
+    call.b.branch = 0
+    got = call.run(("pre_weight", "pre_bias"), ("dy", "dpre_weight", "dpre_bias", "dpost_weight", "dpost_bias"))
+    assert not got["dpost_weight"].any() and not got["dpost_bias"].any()
+    x, w, c = (call.mem[k].clone().requires_grad_(True) for k in ("x", "pre_weight", "pre_bias"))
+    _, y = mx.residual_norm(x, pre_weight=w, pre_bias=c if norm else None, norm="layer" if norm else "rms")
+    want = torch.autograd.grad(y, [x, w] + ([c] if norm else []), call.mem["dy"])
+    # one scale of 1 in both: the residual's is not used without a block
+    for k, t in zip(("dx", "dpre_weight", "dpre_bias"), want):
+        assert torch.equal(got[k], t), k
+    assert norm or not got["dpre_bias"].any()
+
+
+def test_saved_input_of_a_norm_alone(mx):
+    x = torch.randn((96, 64), device="cuda", requires_grad=True)
+    for change, fits in ((torch.clone, True), (lambda t: t.t().contiguous(), False), (lambda t: t[:95], False), (lambda t: t.to(BF), False)):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: change(t) if t.shape == x.shape else t):
+            _, y = mx.residual_norm(x)
+        if fits:
+            torch.autograd.grad(y.sum(), x)
+        else:
+            with pytest.raises(mx.MxError):
+                torch.autograd.grad(y.sum(), x)
